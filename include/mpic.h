@@ -26,6 +26,7 @@
  *     current when the call is made; pointers documented "host" are ordinary host
  *     memory unless "pinned" is stated.
  *   - A context and its plans may be used from one host thread at a time.
+ *   - Norms and positions of fresh rows, and contexts held in 4 bits: mpic_q4.h.
  */
 #ifndef MPIC_H
 #define MPIC_H

@@ -37,6 +37,10 @@ Pin status of every function (see tests/test_oracle_*.py):
                          plan of a text span of the same length, all caches missing is
                          library SDPA causal prefill of every layer, layers read their own
                          slice
+  held.position_rows     pinned: rope.rotate with one axis, each axis alone, unit mean square
+  held.q4_hold           (this build's own format) pinned: hand-coded group, nearest of the
+                         sixteen values by brute force, least value kept
+  held.q4_attend         pinned: attend.attend on the held values
 The paper prints no worked numeric example of this path, so beyond those pins the
 values are unpinned by the paper itself.
 """
@@ -48,3 +52,4 @@ from .decode import decode_attend       # noqa: F401
 from .select import k_distance, top_tokens, top_counts  # noqa: F401
 from .store import ChunkStore            # noqa: F401
 from .pipeline import plan_with_lookup, prefill_layers  # noqa: F401
+from .held import position_rows, q4_attend, q4_hold  # noqa: F401

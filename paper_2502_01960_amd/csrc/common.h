@@ -154,6 +154,9 @@ struct mpic_ctx {
   // plan tables: blocks kept for reuse, and the stream that uploads them (see upload_plan)
   std::shared_ptr<mpic::SpareBlocks> spare_blocks = std::make_shared<mpic::SpareBlocks>();
   hipStream_t upload_stream = nullptr;
+  // rotary base as fractions of a turn per position, in units of 2^-64 (position.hip), once computed
+  bool turns_known = false;
+  uint64_t turns[64] = {};
 };
 
 struct mpic_plan {

@@ -1,0 +1,475 @@
+"""Contexts held in 4 bits: writing, reading back, attention, against the float64 oracle (needs an MI355X)."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2502_01960_amd as mpic
+from oracle import q4_attend, q4_hold
+from oracle.held import round_bf16, round_f32
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def _dt(bf16):
+    return torch.bfloat16 if bf16 else torch.float32
+
+
+def _ctx(hq, hkv, d, bf16):
+    return mpic.Context(hq, hkv, d, mpic.MPIC_BF16 if bf16 else mpic.MPIC_F32, 1e4)
+
+
+def _cache(ctx, n_slots):
+    return torch.full((mpic.mpic_q4_bytes(ctx.handle, n_slots),), 0xA5, dtype=torch.uint8, device=DEV)
+
+
+def _i32(x):
+    return torch.as_tensor(np.asarray(x), dtype=torch.int32).to(DEV)
+
+
+def _rows(n, hkv, d, bf16, seed):
+    """Rows with channels far from zero, scales from 1e-3 to 1e3 and a flat group."""
+    gen = torch.Generator().manual_seed(seed)
+    x = torch.randn((n, hkv, d), generator=gen) * 10.0 ** (3 * torch.rand((n, hkv, 1), generator=gen) - 1.5)
+    x += 2 * torch.randn((1, hkv, d), generator=gen)
+    if n:
+        x[n // 2, 0, :64] = -0.75
+    return x.to(_dt(bf16))
+
+
+def _read_back(x, bf16):
+    value = round_f32(q4_hold(x.double().numpy(), bf16)[0])
+    return round_bf16(value) if bf16 else value
+
+
+# ---------------------------------------------------------------- rows
+@pytest.mark.parametrize("kind", ["bf16", "f32_128", "f32_64"])
+@pytest.mark.parametrize("n", [1, 3, 4, 15, 16, 17, 64, 65, 1001])
+@pytest.mark.parametrize("how", ["in_order", "shuffled", "offset", "none"])
+def test_rows_come_back_as_their_codes_say(kind, n, how):
+    """Exactly: codes, scales and the roundings of the values are whole-number business or correctly rounded."""
+    bf16, d, hkv = kind == "bf16", 64 if kind == "f32_64" else 128, 1 + n % 5
+    ctx = _ctx(2 * hkv, hkv, d, bf16)
+    n_slots = 2 * n + 19
+    rng = np.random.default_rng(n)
+    slots = {"in_order": np.arange(n) + 16, "shuffled": rng.permutation(n_slots)[:n], "offset": np.arange(n) + 3,
+             "none": None}[how]
+    if how == "in_order" and n_slots < n + 16:
+        n_slots = n + 16
+    k, v = _rows(n, hkv, d, bf16, n), _rows(n, hkv, d, bf16, n + 1)
+    cache = _cache(ctx, n_slots)
+    s = None if slots is None else _i32(slots)
+    mpic.mpic_q4_write(ctx.handle, k.to(DEV), v.to(DEV), s, cache, n_slots)
+    ko, vo = (torch.full(k.shape, float("nan"), dtype=_dt(bf16), device=DEV) for _ in range(2))
+    mpic.mpic_q4_read(ctx.handle, cache, n_slots, s, ko, vo)
+    torch.cuda.synchronize()
+    for x, got in ((k, ko), (v, vo)):
+        assert np.array_equal(got.double().cpu().numpy(), _read_back(x, bf16))
+
+
+@pytest.mark.parametrize("bf16", [True, False])
+def test_borders_between_codes(bf16):
+    """Values on, next to and between the borders, with scales that are powers of two and thirds."""
+    rng = np.random.default_rng(7)
+    n, d = 512, 128
+    step = 2.0 ** rng.integers(-20, 20, (n, 1, 2, 1)) * rng.choice([1.0, 1.5, 4 / 3], (n, 1, 2, 1))
+    x = (rng.integers(0, 31, (n, 1, 2, 64)) / 2 + rng.choice([0, 2.0 ** -7, -2.0 ** -7, 2.0 ** -22], (n, 1, 2, 64))) * step
+    x[..., 0], x[..., 1] = 0, 15 * step[..., 0]
+    x = torch.from_numpy(x.reshape(n, 1, d)).to(_dt(bf16))
+    ctx = _ctx(1, 1, d, bf16)
+    cache = _cache(ctx, n)
+    out = torch.empty_like(x, device=DEV)
+    out2 = torch.empty_like(out)
+    mpic.mpic_q4_write(ctx.handle, x.to(DEV), x.to(DEV), None, cache, n)
+    mpic.mpic_q4_read(ctx.handle, cache, n, None, out, out2)
+    want = _read_back(x, bf16)
+    assert np.array_equal(out.double().cpu().numpy(), want) and np.array_equal(out2.double().cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("bf16", [True, False])
+def test_groups_that_are_not_finite_flat_or_tiny(bf16):
+    n = 21
+    x = torch.randn((n, 2, 128), generator=torch.Generator().manual_seed(3)).to(_dt(bf16))
+    x[0, 0, 3], x[1, 1, 70], x[2, 0, 127] = float("nan"), float("inf"), -float("inf")
+    x[3, 0, :64] = 0
+    x[4, 1, 64:] = 2.0 ** -120 * torch.arange(64)
+    x[5, 0, 0], x[5, 0, 1] = 3e38, -3e38
+    x[20, 1, :64] = float("nan")
+    ctx = _ctx(4, 2, 128, bf16)
+    cache = _cache(ctx, n)
+    ko, vo = (torch.zeros_like(x, device=DEV) for _ in range(2))
+    mpic.mpic_q4_write(ctx.handle, x.to(DEV), x.flip(0).contiguous().to(DEV), None, cache, n)
+    mpic.mpic_q4_read(ctx.handle, cache, n, None, ko, vo)
+    want = _read_back(x, bf16)
+    assert np.array_equal(ko.double().cpu().numpy(), want, equal_nan=True)
+    assert np.array_equal(vo.double().cpu().numpy(), want[::-1], equal_nan=True)
+    assert np.isnan(want[0, 0, :64]).all() and np.isfinite(want[0, 0, 64:]).all() and np.isfinite(want[0, 1]).all()
+
+
+@pytest.mark.parametrize("bf16", [True, False])
+def test_rows_without_a_slot_and_other_slots_are_left_alone(bf16):
+    n, n_slots, hkv, d = 37, 50, 3, 128
+    ctx = _ctx(3, hkv, d, bf16)
+    first, k, v = _rows(n_slots, hkv, d, bf16, 1), _rows(n, hkv, d, bf16, 2), _rows(n, hkv, d, bf16, 3)
+    cache = _cache(ctx, n_slots)
+    mpic.mpic_q4_write(ctx.handle, first.to(DEV), first.to(DEV), None, cache, n_slots)
+    slots = np.random.default_rng(4).permutation(n_slots)[:n]
+    slots[[0, 5, 17, 36]] = [-1, n_slots, 2 ** 31 - 1, -2 ** 31]
+    mpic.mpic_q4_write(ctx.handle, k.to(DEV), v.to(DEV), _i32(slots), cache, n_slots)
+    ko, vo = (torch.empty((n_slots, hkv, d), dtype=_dt(bf16), device=DEV) for _ in range(2))
+    mpic.mpic_q4_read(ctx.handle, cache, n_slots, None, ko, vo)
+    for x, got in ((k, ko), (v, vo)):
+        want, rows = _read_back(first, bf16), _read_back(x, bf16)
+        for r, s in enumerate(slots):
+            if 0 <= s < n_slots:
+                want[s] = rows[r]
+        assert np.array_equal(got.double().cpu().numpy(), want)
+    part = torch.full((n, hkv, d), 9.0, dtype=_dt(bf16), device=DEV)
+    part2 = part.clone()
+    mpic.mpic_q4_read(ctx.handle, cache, n_slots, _i32(slots), part, part2)
+    for r, s in enumerate(slots):
+        if not 0 <= s < n_slots:
+            assert (part[r] == 9).all() and (part2[r] == 9).all()
+        else:
+            assert torch.equal(part[r], ko[s]) and torch.equal(part2[r], vo[s])
+    # one slot into several rows
+    same = _i32([7] * n)
+    mpic.mpic_q4_read(ctx.handle, cache, n_slots, same, part, part2)
+    assert all(torch.equal(part[r], ko[7]) and torch.equal(part2[r], vo[7]) for r in range(n))
+
+
+def test_rows_of_a_projection():
+    """k and v as parts of wider rows, and read back into parts of wider rows."""
+    n, hkv, d = 70, 2, 128
+    ctx = _ctx(4, hkv, d, True)
+    wide = _rows(n, 8, d, True, 5).to(DEV)
+    cache = _cache(ctx, n)
+    mpic.mpic_q4_write(ctx.handle, wide[:, 4:6], wide[:, 6:], None, cache, n)
+    back = torch.full_like(wide, 5.0)
+    mpic.mpic_q4_read(ctx.handle, cache, n, None, back[:, 1:3], back[:, 5:7])
+    assert np.array_equal(back[:, 1:3].double().cpu().numpy(), _read_back(wide[:, 4:6].cpu(), True))
+    assert np.array_equal(back[:, 5:7].double().cpu().numpy(), _read_back(wide[:, 6:].cpu(), True))
+    assert (back[:, [0, 3, 4, 7]] == 5).all()
+
+
+def test_cache_past_4_gib():
+    hkv, d = 8, 128
+    ctx = _ctx(8, hkv, d, True)
+    n_slots = (1 << 32) // (144 * hkv) + 40000
+    assert mpic.mpic_q4_bytes(ctx.handle, n_slots) > 1 << 32
+    cache = torch.zeros(mpic.mpic_q4_bytes(ctx.handle, n_slots), dtype=torch.uint8, device=DEV)
+    k, v = _rows(96, hkv, d, True, 8), _rows(96, hkv, d, True, 9)
+    page, lens = 16, [90]
+    pages = [n_slots // 16 - 1 - i for i in range(3)] + [0, 5, n_slots // 32]
+    slots = np.concatenate([np.arange(16) + 16 * p for p in pages])
+    mpic.mpic_q4_write(ctx.handle, k.to(DEV), v.to(DEV), _i32(slots), cache, n_slots)
+    ko, vo = (torch.empty(k.shape, dtype=k.dtype, device=DEV) for _ in range(2))
+    mpic.mpic_q4_read(ctx.handle, cache, n_slots, _i32(slots), ko, vo)
+    assert np.array_equal(ko.double().cpu().numpy(), _read_back(k, True)) and np.array_equal(vo.double().cpu().numpy(), _read_back(v, True))
+    q = torch.randn((1, 8, d), generator=torch.Generator().manual_seed(1)).to(torch.bfloat16).to(DEV)
+    out, near = torch.empty_like(q), torch.empty_like(q)
+    _attend(ctx, q, cache, n_slots, _i32([pages]), page, _i32(lens), out)
+    small = _cache(ctx, 96)
+    mpic.mpic_q4_write(ctx.handle, k.to(DEV), v.to(DEV), None, small, 96)
+    _attend(ctx, q, small, 96, _i32([[0, 1, 2, 3, 4, 5]]), page, _i32(lens), near)
+    assert torch.equal(out, near)
+
+
+# ---------------------------------------------------------------- attention
+def _attend(ctx, q, cache, n_slots, table, page, lens, out, lse=None, q_off=None, max_q=1, max_len=None, scale=None):
+    bound = table.shape[1] * page if max_len is None else max_len
+    size = mpic.mpic_q4_attn_workspace(ctx.handle, table.shape[0], q.shape[0], max_q, bound)
+    ws = torch.full((max(size, 1),), 0xFF, dtype=torch.uint8, device=DEV)     # (NaN where it is read unwritten)
+    mpic.mpic_q4_attn(ctx.handle, q, cache, n_slots, table, page, lens, scale or 1 / math.sqrt(ctx.head_dim), out, lse, q_off, max_q,
+                      max_len, ws)
+    torch.cuda.synchronize()
+
+
+class Held:
+    """Requests with their contexts in a paged cache, shuffled pages, codes of another content everywhere else."""
+
+    def __init__(self, lens, news, hq, hkv, d, bf16, page=16, seed=0, spread=1.0):
+        self.lens, self.news, self.d, self.bf16, self.page = lens, news, d, bf16, page
+        self.ctx = _ctx(hq, hkv, d, bf16)
+        gen = torch.Generator().manual_seed(seed + sum(lens))
+        dt = _dt(bf16)
+        self.bias = 2 * torch.randn((1, hkv, d), generator=gen)
+        self.k = [(torch.randn((n, hkv, d), generator=gen) + self.bias).to(dt) for n in lens]
+        self.v = [torch.randn((n, hkv, d), generator=gen).to(dt) for n in lens]
+        self.q = (torch.randn((sum(news), hq, d), generator=gen) * spread).to(dt)
+        need = [-(-n // page) for n in lens]
+        self.n_pages = sum(need) + 3
+        order = np.random.default_rng(seed).permutation(self.n_pages)
+        self.table = np.full((len(lens), max(need + [1]) + 1), -7)
+        at = 0
+        for b, n in enumerate(need):
+            self.table[b, :n] = order[at:at + n]
+            at += n
+        self.n_slots = self.n_pages * page
+        self.cache = _cache(self.ctx, self.n_slots)       # 0xA5 everywhere: codes and pairs of no meaning
+        for b, n in enumerate(lens):
+            if n:
+                j = np.arange(n)
+                mpic.mpic_q4_write(self.ctx.handle, self.k[b].to(DEV), self.v[b].to(DEV),
+                                   _i32(self.table[b, j // page] * page + j % page), self.cache, self.n_slots)
+        self.q_off = np.concatenate([[0], np.cumsum(news)])
+
+    def run(self, max_len=None, max_q=None, q_off=True, lse=True):
+        q = self.q.to(DEV)
+        out = torch.full(self.q.shape, 77.0, dtype=_dt(self.bf16), device=DEV)
+        l = torch.full(self.q.shape[:2], 77.0, dtype=torch.float32, device=DEV) if lse else None
+        _attend(self.ctx, q, self.cache, self.n_slots, _i32(self.table), self.page, _i32(self.lens), out, l,
+                _i32(self.q_off) if q_off else None, max_q or max(self.news + [1]) if q_off else 1, max_len)
+        return out.double().cpu().numpy(), None if l is None else l.double().cpu().numpy()
+
+    def check(self, out, lse, lens=None):
+        lens = self.lens if lens is None else lens
+        scale = 1 / math.sqrt(self.d)
+        held = [[q4_hold(x.double().numpy(), self.bf16) for x in side] for side in (self.k, self.v)]
+        q = self.q.double().numpy()
+        ref, ref_lse = q4_attend(q, [h[0] for h in held[0]], [h[0] for h in held[1]], lens, self.news, scale)
+        # Scores: 128 products of a query value with a code below 16 and the sum of the queries, in fp32, times a scale; 2^-21
+        # holds the roundings of some eight additions of partial sums.  A score off by e moves an output by 2 e max|v| at most.
+        step = max([float(np.nanmax(h[2])) for h in held[0] if h[2].size] + [0.0])
+        score = 2.0 ** -21 * scale * 32 * step * np.abs(q).sum(-1, keepdims=True)
+        top = max([float(np.abs(h[0]).max()) for h in held[1] if h[0].size] + [0.0])
+        # Weights times a scale of V are rounded once (bf16 2^-8; f32: three parts, 2^-24) and meet codes up to 8 from the middle
+        # (f32: up to 15)
+        spread = max([float((8 if self.bf16 else 15) * h[2].max()) for h in held[1] if h[2].size] + [0.0])
+        tol = 2 * score * top + (2.0 ** -8 if self.bf16 else 2.0 ** -22) * (np.abs(ref) + spread)
+        err = np.abs(out - ref)
+        assert (err <= tol).all(), float((err / np.maximum(tol, 1e-30)).max())
+        # a rounding is uniform within its half step h, so its root mean square is h / sqrt(3), that of a sum of independent
+        # ones at most the sum of theirs, and a mean at most the root mean square
+        assert err.mean() <= tol.mean() / math.sqrt(3)
+        if lse is not None:
+            seen = np.isfinite(ref_lse)
+            assert np.array_equal(lse[~seen], ref_lse[~seen])
+            assert (np.abs(lse[seen] - ref_lse[seen]) <= score[..., 0][seen] + 2.0 ** -20 * (1 + np.abs(ref_lse[seen]))).all()
+
+
+MODELS = [(4, 4, 128, True), (28, 4, 128, True), (8, 1, 128, True), (40, 2, 128, True), (6, 2, 128, False), (4, 4, 64, False)]
+
+
+@pytest.mark.parametrize("model", MODELS)
+@pytest.mark.parametrize("lens", [[1], [15, 16, 17], [31, 0, 32, 33], [128, 129, 1], [300, 777], [2049]])
+def test_one_query_per_request(model, lens):
+    p = Held(lens, [1] * len(lens), *model)
+    out, lse = p.run(q_off=False)
+    p.check(out, lse)
+    assert np.array_equal(out, p.run(q_off=True, lse=False)[0])
+
+
+@pytest.mark.parametrize("model", MODELS)
+@pytest.mark.parametrize("lens,news", [([5], [5]), ([17, 3, 40], [16, 0, 2]), ([200, 64], [33, 64]), ([3, 1], [7, 2]), ([700], [90])])
+def test_several_queries_per_request(model, lens, news):
+    """Requests made of nothing but new tokens, requests without any, more queries than tokens (the first see nothing)."""
+    p = Held(lens, news, *model, page=32)
+    p.check(*p.run())
+
+
+@pytest.mark.parametrize("page", [16, 48, 256])
+def test_pages(page):
+    p = Held([49, 512, 513], [1, 3, 1], 8, 2, 128, True, page=page)
+    p.check(*p.run())
+
+
+@pytest.mark.parametrize("bf16", [True, False])
+def test_long_context_is_split_and_bounds_do_not_change_it(bf16):
+    p = Held([9000, 4097, 2], [1, 1, 1], 8, 2, 128, bf16, page=64)
+    out, lse = p.run(max_len=9000)
+    p.check(out, lse)
+    p.check(*p.run())                                    # a looser bound, other splits
+    p.check(*p.run(max_len=4097), lens=[4097, 4097, 2])  # lengths beyond the bound are cut
+
+
+def test_sharp_and_flat_scores():
+    for spread in (30.0, 0.0):
+        p = Held([1000, 40], [1, 3], 8, 2, 128, True, spread=spread)
+        p.check(*p.run())
+
+
+def test_queries_beyond_max_q_and_rows_of_no_request():
+    p = Held([60, 33], [5, 3], 4, 2, 128, True)
+    full, lse = p.run()
+    p.q_off = np.array([0, 5, 8])
+    out, l = p.run(max_q=4)
+    assert np.array_equal(out[:4], full[:4]) and (out[4] == 77).all() and np.array_equal(out[5:], full[5:]) and (l[4] == 77).all()
+    # rows in front of, between and behind the requests
+    p.q_off = np.array([2, 5, 5])
+    p.news = [3, 0]
+    out, l = p.run()
+    assert (out[:2] == 77).all() and (out[5:] == 77).all() and (l[:2] == 77).all() and (out[2:5] != 77).any()
+
+
+def test_pages_outside_the_cache_and_odd_arrays_are_not_followed():
+    p = Held([64, 64], [1, 1], 4, 2, 128, True)
+    q = p.q.to(DEV)
+    ref, _ = p.run(q_off=False)
+    for wrong in (-1, p.n_pages, 2 ** 31 - 1, -2 ** 31):
+        keep = p.table[0, 2]
+        p.table[0, 2] = wrong
+        out, lse = p.run(q_off=False)
+        p.table[0, 2] = keep
+        assert np.array_equal(out[1], ref[1])
+        # the tokens of that page are not seen
+        seen = np.r_[0:32, 48:64]
+        held = [[q4_hold(x[0].double().numpy()[seen], True)[0]] for x in (p.k, p.v)]
+        want, _ = q4_attend(p.q.double().numpy()[:1], held[0], held[1], [48], [1], 1 / math.sqrt(128))
+        assert np.abs(out[0] - want[0]).max() < 2.0 ** -6
+    # no page at all: zeros
+    out = torch.full_like(q, 5.0)
+    lse = torch.empty(q.shape[:2], device=DEV)
+    _attend(p.ctx, q, p.cache, p.n_slots, _i32(np.full((2, 4), -1)), 16, _i32([64, -3]), out, lse)
+    assert (out == 0).all() and torch.isinf(lse).all() and (lse < 0).all()
+    # query offsets that run backwards or past the rows
+    for off in ([0, 5, 1], [-9, 1, 2 ** 31 - 1], [2, 1, 0]):
+        out = torch.full_like(q, 5.0)
+        _attend(p.ctx, q, p.cache, p.n_slots, _i32(p.table), 16, _i32([64, 64]), out, None, _i32(off), 2)
+
+
+@pytest.mark.parametrize("model", [(8, 2, 128, True), (4, 4, 64, False)])
+def test_what_is_not_finite_stays_with_those_who_see_it(model):
+    p = Held([70, 70], [3, 3], *model, page=32)
+    ref, _ = p.run()
+    d = model[2]
+    # NaN keys and values behind the end of both requests (slots 70 .. 95) and in a page of nobody
+    nan = torch.full((26, model[1], d), float("nan"), dtype=_dt(p.bf16), device=DEV)
+    j = np.arange(70, 96)
+    for b in range(2):
+        mpic.mpic_q4_write(p.ctx.handle, nan, nan, _i32(p.table[b, j // 32] * 32 + j % 32), p.cache, p.n_slots)
+    out, _ = p.run()
+    assert np.array_equal(out, ref)
+    # the value of the last token of request 0, head 0: only its last query sees it
+    v = p.v[0][69:70].clone()
+    v[0, 0, d - 1] = float("inf")
+    slot = _i32(p.table[0, [2]] * 32 + 5)
+    mpic.mpic_q4_write(p.ctx.handle, p.k[0][69:70].to(DEV), v.to(DEV), slot, p.cache, p.n_slots)
+    out, _ = p.run()
+    per = model[0] // model[1]
+    hit = np.isnan(out)
+    assert hit[2, :per, d - 64:].all() and hit.sum() == per * 64
+    assert np.array_equal(out[~hit], ref[~hit])
+    # its key
+    k = p.k[0][69:70].clone()
+    k[0, 0, 0] = float("nan")
+    mpic.mpic_q4_write(p.ctx.handle, k.to(DEV), p.v[0][69:70].to(DEV), slot, p.cache, p.n_slots)
+    out, lse = p.run()
+    hit = np.isnan(out)
+    assert hit[2, :per].all() and hit.sum() == per * d and np.isnan(lse).sum() == per and np.isnan(lse[2, :per]).all()
+
+
+def test_strided_queries():
+    p = Held([100, 9], [1, 1], 8, 2, 128, True)
+    ref, _ = p.run(q_off=False)
+    wide = torch.zeros((2, 12, 128), dtype=torch.bfloat16, device=DEV)
+    wide[:, :8] = p.q.to(DEV)
+    out = torch.empty((2, 8, 128), dtype=torch.bfloat16, device=DEV)
+    _attend(p.ctx, wide[:, :8], p.cache, p.n_slots, _i32(p.table), 16, _i32(p.lens), out)
+    assert np.array_equal(out.double().cpu().numpy(), ref)
+
+
+def test_repeats_are_identical_and_streams_do_not_meet():
+    p = Held([3000, 1200], [1, 2], 28, 4, 128, True, page=64)
+    ref, _ = p.run()
+    for _ in range(3):
+        assert np.array_equal(p.run()[0], ref)
+    other = Held([2000, 2000], [2, 1], 28, 4, 128, True, page=64, seed=9)
+    other.ctx = p.ctx
+    want, _ = other.run()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    work = []
+    for x in (p, other):
+        q, t, l, o = x.q.to(DEV), _i32(x.table), _i32(x.lens), _i32(x.q_off)
+        size = mpic.mpic_q4_attn_workspace(p.ctx.handle, 2, 3, 2, x.table.shape[1] * 64)
+        work.append((x, q, t, l, o, torch.empty_like(q), torch.empty(size, dtype=torch.uint8, device=DEV)))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for s, (x, q, t, l, o, out, ws) in zip(streams, work):
+            mpic.mpic_q4_attn(p.ctx.handle, q, x.cache, x.n_slots, t, 64, l, 1 / math.sqrt(128), out, None, o, 2, None, ws, s)
+    torch.cuda.synchronize()
+    for (x, q, t, l, o, out, ws), r in zip(work, (ref, want)):
+        assert np.array_equal(out.double().cpu().numpy(), r)
+
+
+# ---------------------------------------------------------------- together
+def test_generation_over_a_linked_context_from_one_graph():
+    """Link a context, hold it in 4 bits, then generate: position the new rows, write them, attend; captured once, replayed for
+    every token with other inputs, other lengths and eager work in between."""
+    import workloads
+    from helpers import Problem
+    prob = Problem(3, n_chunks=2, chunk_len=130, text_len=21, batch=2)
+    prob.gpu_setup(False)
+    prob.gpu_assemble()
+    sh, ctx = prob.sh, prob.ctx
+    off = prob.oplan["ctx_off"]
+    lens = [int(off[b + 1] - off[b]) for b in range(2)]
+    page, steps = 64, 5
+    width = -(-(max(lens) + steps) // page)
+    n_slots = 2 * width * page
+    table = np.random.default_rng(0).permutation(2 * width).reshape(2, width)
+    slot = lambda b, j: int(table[b, j // page] * page + j % page)
+    cache = _cache(ctx, n_slots)
+    where = _i32([slot(b, j) for b in range(2) for j in range(lens[b])])
+    mpic.mpic_q4_write(ctx.handle, prob.k_ctx[:sum(lens)], prob.v_ctx[:sum(lens)], where, cache, n_slots)
+    hq, hkv, d = sh.n_q_heads, sh.n_kv_heads, sh.head_dim
+    dt = torch.bfloat16
+    rows = torch.zeros((2, hq + 2 * hkv, d), dtype=dt, device=DEV)       # a projection's output
+    pos, slots, d_lens = (torch.zeros(2, dtype=torch.int32, device=DEV) for _ in range(3))
+    q, k, out = (torch.zeros((2, h, d), dtype=dt, device=DEV) for h in (hq, hkv, hq))
+    w = torch.ones(d, dtype=dt, device=DEV)
+    d_table = _i32(table)
+    ws = torch.empty(max(1, mpic.mpic_q4_attn_workspace(ctx.handle, 2, 2, 1, width * page)), dtype=torch.uint8, device=DEV)
+
+    def step():
+        mpic.mpic_position_rows(ctx.handle, rows[:, :hq], rows[:, hq:hq + hkv], pos, q, k, w, w, 1e-6)
+        mpic.mpic_q4_write(ctx.handle, k, rows[:, hq + hkv:], slots, cache, n_slots)
+        mpic.mpic_q4_attn(ctx.handle, q, cache, n_slots, d_table, page, d_lens, sh.softmax_scale, out, workspace=ws)
+
+    gen = torch.Generator().manual_seed(5)
+    inputs = [torch.randn(rows.shape, generator=gen).to(dt) for _ in range(steps)]
+
+    def feed(i):
+        rows.copy_(inputs[i])
+        pos.copy_(_i32([n + i for n in lens]))
+        slots.copy_(_i32([slot(b, lens[b] + i) for b in range(2)]))
+        d_lens.copy_(_i32([n + i + 1 for n in lens]))
+
+    eager = []
+    for i in range(steps):
+        feed(i)
+        step()
+        torch.cuda.synchronize()
+        eager.append((out.clone(), cache.clone()))
+    start = eager[0][1].clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    cache.fill_(0xA5)
+    mpic.mpic_q4_write(ctx.handle, prob.k_ctx[:sum(lens)], prob.v_ctx[:sum(lens)], where, cache, n_slots)
+    for i in range(steps):
+        feed(i)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager[i][0]) and torch.equal(cache, eager[i][1]), i
+        torch.randn(1000, device=DEV).sum().item()
+    assert not torch.equal(start, cache)
+    # the last step against the oracle, over what the cache holds
+    K, V = prob.oracle_link()
+    from oracle import position_rows
+    from oracle.held import round_bf16 as r16
+    for b in range(2):
+        kk, vv = [K[off[b]:off[b + 1]]], [V[off[b]:off[b + 1]]]
+        for i in range(steps):
+            x = inputs[i][b:b + 1].double().numpy()
+            kk.append(r16(position_rows(x[:, hq:hq + hkv], [[lens[b] + i]], sh.rope_theta, eps=1e-6)))
+            vv.append(x[:, hq + hkv:])
+        x = inputs[-1][b:b + 1].double().numpy()
+        qq = r16(position_rows(x[:, :hq], [[lens[b] + steps - 1]], sh.rope_theta, eps=1e-6))
+        held = [q4_hold(r16(np.concatenate(y)), True)[0] for y in (kk, vv)]
+        want, _ = q4_attend(qq, [held[0]], [held[1]], [lens[b] + steps], [1], sh.softmax_scale)
+        got = out[b].double().cpu().numpy()
+        # a key whose bf16 rounding falls the other way may take the next code: one key of several hundred
+        assert np.abs(got - want[0]).max() <= 2e-2 and np.abs(got - want[0]).mean() <= 2e-3
