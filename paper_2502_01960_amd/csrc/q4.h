@@ -1,13 +1,13 @@
 // Layout of a cache held in 4 bits, shared by the kernels that write, read and attend it.
 //
 // 16 slots and one kv head make a block; blocks lie slot group after slot group, inside it head after head.  A block holds
-//   K codes   [16 tokens][4 quarters][D / 8 bytes]   quarter c of a token: per group of 64 values the 16 values 16c .. 16c + 15
+//   K codes   [4 quarters][16 tokens][D / 8 bytes]   quarter c of a token: per group of 64 values the 16 values 16c .. 16c + 15
 //   V codes   [4 token quads][16 columns][D / 8 bytes]  column i of tokens 4g .. 4g + 3: per group the values 4i .. 4i + 3
 //   K pairs   [D / 64 groups][16 tokens] (scale, low)
 //   V pairs   the same
-// so that a wavefront of the attention kernel fetches the K codes of 16 tokens with one load, D / 8 bytes a lane, and finds
-// in every lane what a 16x16x32 matrix instruction takes from that lane: of K eight neighbouring values of one token, of
-// V (whose tokens are the summed dimension) four tokens of one column.  No transposition and no LDS on the way.
+// so that lane after lane of a wavefront reads D / 8 bytes after D / 8 bytes, of K and of V, and finds there what a 16x16x32
+// matrix instruction takes from that lane: of K eight neighbouring values of one token, of V (whose tokens are the summed
+// dimension) four tokens of one column.  Nothing is transposed on the way.
 // A K word holds 8 neighbouring values, value 2n in bits 4n.. and value 2n + 1 in bits 16 + 4n..; a V word holds two
 // columns of four tokens, token r in byte r, the even column in its low half.
 #pragma once

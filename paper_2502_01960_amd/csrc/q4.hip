@@ -124,7 +124,7 @@ __device__ inline void write_keys(const RowsArgs& a, int64_t row0, int head, int
       reinterpret_cast<Pair<T>*>(block + B::kKPairs)[g * kTokens + (slot & 15)] = Pair<T>{static_cast<T>(code.scale), static_cast<T>(code.low)};
   }
   if (slot < 0) return;
-  uint32_t* dst = reinterpret_cast<uint32_t*>(block + ((slot & 15) * 4 + c) * B::kLaneBytes);
+  uint32_t* dst = reinterpret_cast<uint32_t*>(block + (c * kTokens + (slot & 15)) * B::kLaneBytes);
 #pragma unroll
   for (int w = 0; w < B::kGroups * 2; ++w) dst[w] = words[w];
 }
@@ -211,7 +211,7 @@ __global__ __launch_bounds__(256) void q4_read_kernel(RowsArgs a) {
     const int slot = slot_of(a, item.row0 + t);
     if (slot < 0) return;
     const char* block = block_of<T, D>(a, slot, item.head);
-    const uint32_t* src = reinterpret_cast<const uint32_t*>(block + ((slot & 15) * 4 + c) * B::kLaneBytes);
+    const uint32_t* src = reinterpret_cast<const uint32_t*>(block + (c * kTokens + (slot & 15)) * B::kLaneBytes);
     char* dst = const_cast<char*>(a.k) + (item.row0 + t) * a.k_stride + (item.head * D + 16 * c) * sizeof(T);
 #pragma unroll
     for (int g = 0; g < B::kGroups; ++g) {

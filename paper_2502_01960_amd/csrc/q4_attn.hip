@@ -18,6 +18,8 @@
 //
 // A workgroup of four wavefronts takes a split of a request's keys for one kv head and 16 rows; its wavefronts take the
 // units in turn and meet in LDS at the end.  Where the keys are cut into several splits, a second launch merges them.
+// The kernel is bound by HBM bandwidth as long as enough loads are in flight: every wavefront has two units of LDS of its
+// own, filled by direct global->LDS loads (five a unit, no registers, no barrier) while it works on the other one.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -126,27 +128,59 @@ struct Shape {
   static constexpr float kCode = kExact ? 1.f : 16.f;  // what a product with the codes has to be multiplied with
 };
 
-// What a lane holds of a block: codes, and the pairs of its four tokens
+// A unit in LDS: the codes of its two blocks (K, then V), then the pairs of the first block (K, V), then of the second
+template <typename T, int D>
+struct Unit {
+  using B = Block<T, D>;
+  static constexpr int kCodes = 2 * B::kCodes;         // of a block
+  static constexpr int kPairs = 2 * B::kPairs;
+  static constexpr int kBytes = 2 * (kCodes + kPairs);
+  static constexpr int kLoads = 2 * (kCodes / 1024) + 1;  // direct loads of a wavefront
+  static_assert(kCodes % 1024 == 0 && 2 * kPairs <= 1024, "whole wavefronts load the codes, part of one the pairs");
+};
 template <typename T, int D>
 struct Held {
   typedef uint32_t words __attribute__((ext_vector_type(Shape<T, D>::kWords)));
   typedef T pairs __attribute__((ext_vector_type(8)));  // scale, low of four tokens
-  words k, v;
-  pairs kp[Shape<T, D>::kGroups], vp[Shape<T, D>::kGroups];
 };
+// Block b's codes (kV: of V) and pairs of group g in this lane
+template <typename T, int D, bool kV>
+__device__ inline typename Held<T, D>::words codes_in(const char* unit, int b, int lane) {
+  using U = Unit<T, D>;
+  return *reinterpret_cast<const typename Held<T, D>::words*>(unit + b * U::kCodes + (kV ? U::B::kV : 0) + lane * U::B::kLaneBytes);
+}
+template <typename T, int D, bool kV>
+__device__ inline typename Held<T, D>::pairs pairs_in(const char* unit, int b, int g, int quarter) {
+  using U = Unit<T, D>;
+  return *reinterpret_cast<const typename Held<T, D>::pairs*>(unit + 2 * U::kCodes + b * U::kPairs + (kV ? U::B::kPairs : 0) +
+                                                              (g * kTokens + 4 * quarter) * U::B::kPair);
+}
+
+// Direct loads of 1024 and 2 x 1024 contiguous bytes to LDS, 16 a lane: base in scalar registers, the lane's offset in one
+// vector register (an instruction's offset moves both addresses).  No compiler-visible load: the wait is by hand.
+__device__ inline void stage_1k(const char* base, uint32_t offset, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(offset), "s"(base), "s"(lds) : "memory", "m0");
+}
+__device__ inline void stage_2k(const char* base, uint32_t offset, uint32_t lds) {
+  asm volatile(
+      "s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1\n\tglobal_load_lds_dwordx4 %0, %1 offset:1024"
+      :
+      : "v"(offset), "s"(base), "s"(lds)
+      : "memory", "m0");
+}
 template <typename T, int D>
-__device__ inline Held<T, D> load_block(const char* block, int lane) {
-  using B = Block<T, D>;
-  using H = Held<T, D>;
-  H h;
-  h.k = *reinterpret_cast<const typename H::words*>(block + ((lane & 15) * 4 + (lane >> 4)) * B::kLaneBytes);
-  h.v = *reinterpret_cast<const typename H::words*>(block + B::kV + lane * B::kLaneBytes);
-#pragma unroll
-  for (int g = 0; g < B::kGroups; ++g) {
-    h.kp[g] = *reinterpret_cast<const typename H::pairs*>(block + B::kKPairs + (g * kTokens + 4 * (lane >> 4)) * B::kPair);
-    h.vp[g] = *reinterpret_cast<const typename H::pairs*>(block + B::kVPairs + (g * kTokens + 4 * (lane >> 4)) * B::kPair);
+__device__ inline void stage_unit(const char* block0, const char* block1, int lane, uint32_t lds) {
+  using U = Unit<T, D>;
+  constexpr int kLanes = U::kPairs / 16;  // lanes that load the pairs of a block
+  if (U::kCodes == 2048) {
+    stage_2k(block0, 16 * lane, lds);
+    stage_2k(block1, 16 * lane, lds + U::kCodes);
+  } else {
+    stage_1k(block0, 16 * lane, lds);
+    stage_1k(block1, 16 * lane, lds + U::kCodes);
   }
-  return h;
+  if (lane < 2 * kLanes)
+    load_to_lds_16B((lane < kLanes ? block0 : block1) + U::kCodes + 16 * (lane % kLanes), lds + 2 * U::kCodes);
 }
 
 __device__ inline f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
@@ -166,26 +200,29 @@ struct Columns {
 
 // One unit of 32 tokens.  kMasked: not every token is seen by every column (or a block is missing: bit of `have`).
 template <typename T, int D, bool kMasked>
-__device__ inline void attend_unit(Columns<T, D>& s, const Held<T, D> (&h)[2], int pos, int have, int quarter, float factor) {
+__device__ inline void attend_unit(Columns<T, D>& s, const char* unit, int pos, int have, int lane, float factor) {
   using S = Shape<T, D>;
+  const int quarter = lane >> 4;
   float x[2][4];
 #pragma unroll
   for (int b = 0; b < 2; ++b) {
     f32x4 sum = f32x4{0};
+    const typename Held<T, D>::words words = codes_in<T, D, false>(unit, b, lane);
 #pragma unroll
     for (int g = 0; g < S::kGroups; ++g) {
+      const typename Held<T, D>::pairs pairs = pairs_in<T, D, false>(unit, b, g, quarter);
       const float start = S::kExact ? 0.f : -s.q_sum[g];
       f32x4 acc = {start, start, start, start};
 #pragma unroll
       for (int w = 0; w < 2; ++w) {
-        const bf16x8 codes = keys_of<S::kExact>(h[b].k[2 * g + w]);
+        const bf16x8 codes = keys_of<S::kExact>(words[2 * g + w]);
 #pragma unroll
         for (int i = 0; i < S::kParts; ++i) acc = mfma(codes, s.q[g][w].p[i], acc);
       }
       const float base = s.q_sum[g] * (1.f / S::kCode);
 #pragma unroll
       for (int r = 0; r < 4; ++r)
-        sum[r] = fmaf(static_cast<float>(h[b].kp[g][2 * r]), acc[r], fmaf(static_cast<float>(h[b].kp[g][2 * r + 1]), base, sum[r]));
+        sum[r] = fmaf(static_cast<float>(pairs[2 * r]), acc[r], fmaf(static_cast<float>(pairs[2 * r + 1]), base, sum[r]));
     }
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
@@ -221,19 +258,22 @@ __device__ inline void attend_unit(Columns<T, D>& s, const Held<T, D> (&h)[2], i
       p[b][r] = __builtin_amdgcn_exp2f(fmaf(x[b][r], factor, -m));
       s.l += p[b][r];
     }
+  const typename Held<T, D>::words v0 = codes_in<T, D, true>(unit, 0, lane), v1 = codes_in<T, D, true>(unit, 1, lane);
 #pragma unroll
   for (int g = 0; g < S::kGroups; ++g) {
     f32x8 w;
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
+    for (int b = 0; b < 2; ++b) {
+      const typename Held<T, D>::pairs pairs = pairs_in<T, D, true>(unit, b, g, quarter);
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        float scaled = p[b][r] * static_cast<float>(h[b].vp[g][2 * r]);
-        float low = p[b][r] * static_cast<float>(h[b].vp[g][2 * r + 1]);
+        float scaled = p[b][r] * static_cast<float>(pairs[2 * r]);
+        float low = p[b][r] * static_cast<float>(pairs[2 * r + 1]);
         if (kMasked && x[b][r] == -INFINITY) scaled = low = 0.f;  // (what is not seen may be no number)
         w[4 * b + (r & 1) * 2 + (r >> 1)] = scaled;               // tokens (0, 2), (1, 3)
         s.low[g] += S::kExact ? low : fmaf(8.f, scaled, low);
       }
+    }
     const Parts<S::kParts> weights = split_parts<S::kParts>(w);
 #pragma unroll
     for (int i = 0; i < S::kParts; ++i) {
@@ -243,20 +283,35 @@ __device__ inline void attend_unit(Columns<T, D>& s, const Held<T, D> (&h)[2], i
       }
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        s.o[g][2 * c] = mfma(values_of<S::kExact, 0>(h[0].v[2 * g + c], h[1].v[2 * g + c]), weights.p[i], s.o[g][2 * c]);
-        s.o[g][2 * c + 1] = mfma(values_of<S::kExact, 1>(h[0].v[2 * g + c], h[1].v[2 * g + c]), weights.p[i], s.o[g][2 * c + 1]);
+        s.o[g][2 * c] = mfma(values_of<S::kExact, 0>(v0[2 * g + c], v1[2 * g + c]), weights.p[i], s.o[g][2 * c]);
+        s.o[g][2 * c + 1] = mfma(values_of<S::kExact, 1>(v0[2 * g + c], v1[2 * g + c]), weights.p[i], s.o[g][2 * c + 1]);
       }
     }
   }
 }
 
+// LDS: the units of every wavefront; at the end their partial results (rows of D + 4 floats, reference points, sums)
 template <typename T, int D>
-__global__ __launch_bounds__(kWaves * 64) void q4_attn_kernel(Q4AttnArgs a) {
+struct AttnLds {
+  static constexpr int kRow = D + 4;
+  static constexpr int kWave = 2 * Unit<T, D>::kBytes;
+  static constexpr int kParts = kWaves * kCols * (kRow + 2) * 4;
+  static constexpr int kBytes = kWaves * kWave > kParts ? kWaves * kWave : kParts;
+  static_assert(kBytes <= 65536, "no opt-in needed");
+};
+
+template <typename T, int D>
+__global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 3 : 2) void q4_attn_kernel(Q4AttnArgs a) {
   using S = Shape<T, D>;
   using B = Block<T, D>;
-  constexpr int kRow = D + 4;  // floats of a row of partial outputs in LDS
-  __shared__ __attribute__((aligned(16))) float part_o[kWaves][kCols][kRow];
-  __shared__ float part_m[kWaves][kCols], part_l[kWaves][kCols];
+  using L = AttnLds<T, D>;
+  using U = Unit<T, D>;
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  typedef float PartRows[kCols][L::kRow];
+  typedef float PartCols[kCols];
+  PartRows* part_o = reinterpret_cast<PartRows*>(lds);
+  PartCols* part_m = reinterpret_cast<PartCols*>(part_o + kWaves);
+  PartCols* part_l = part_m + kWaves;
   const int lane = threadIdx.x & 63, col = lane & 15, quarter = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int split = blockIdx.x, head = blockIdx.y % a.n_kv_heads, b = blockIdx.z;
@@ -310,26 +365,37 @@ __global__ __launch_bounds__(kWaves * 64) void q4_attn_kernel(Q4AttnArgs a) {
       if (id >= 0 && id < a.n_blocks) ids = static_cast<int>(id);
     }
   };
-  auto fetch = [&](int i, Held<T, D>(&h)[2], int* have) {
-    *have = 0;
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const int id = __builtin_amdgcn_readlane(ids, (2 * i & 63) + k);
-      *have |= (id >= 0) << k;
-      h[k] = load_block<T, D>(a.cache + (static_cast<int64_t>(max(id, 0)) * a.n_kv_heads + head) * B::kBytes, lane);
-    }
-  };
-  for (int i = 0; i < n_units; ++i) {
+  char* ring = lds + wave * L::kWave;
+  const uint32_t ring_lds = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(MPIC_LDS_PTR(char, ring)));
+  // load unit i of this wavefront into its half of the ring; bit b of the result: block b is in the cache
+  auto stage = [&](int i) {
     if ((i & 31) == 0) look_up(i);
-    Held<T, D> h[2];
-    int have;
-    fetch(i, h, &have);
+    const int id0 = __builtin_amdgcn_readlane(ids, 2 * i & 63), id1 = __builtin_amdgcn_readlane(ids, (2 * i & 63) + 1);
+    const char* base = a.cache + static_cast<int64_t>(head) * B::kBytes;
+    const int64_t pitch = static_cast<int64_t>(a.n_kv_heads) * B::kBytes;
+    stage_unit<T, D>(base + max(id0, 0) * pitch, base + max(id1, 0) * pitch, lane, ring_lds + (i & 1) * U::kBytes);
+    return (id0 >= 0 ? 1 : 0) | (id1 >= 0 ? 2 : 0);
+  };
+  int have = 0;
+  if (n_units > 0) have = stage(0);
+  for (int i = 0; i < n_units; ++i) {
+    int have_next = 0;
+    if (i + 1 < n_units) {
+      have_next = stage(i + 1);
+      MPIC_WAIT_VMCNT(U::kLoads);
+    } else {
+      MPIC_WAIT_VMCNT(0);
+    }
+    asm volatile("" ::: "memory");
+    const char* unit = ring + (i & 1) * U::kBytes;
     const int pos = (unit0 + i * kWaves) * kUnit;
     if (have == 3 && pos + kUnit <= key_all)
-      attend_unit<T, D, false>(s, h, pos, have, quarter, factor);
+      attend_unit<T, D, false>(s, unit, pos, have, lane, factor);
     else
-      attend_unit<T, D, true>(s, h, pos, have, quarter, factor);
+      attend_unit<T, D, true>(s, unit, pos, have, lane, factor);
+    have = have_next;
   }
+  __syncthreads();
 
   s.l += __shfl_xor(s.l, 16);
   s.l += __shfl_xor(s.l, 32);
@@ -385,50 +451,72 @@ __global__ __launch_bounds__(kWaves * 64) void q4_attn_kernel(Q4AttnArgs a) {
   if (a.lse && threadIdx.x % 16 == 0) a.lse[row] = lse2 * 0.6931471805599453f;
 }
 
-// Output rows from the partial results of their splits: D / 4 threads a row, the splits in their order.
+// Output rows from the partial results of their splits.  A workgroup takes a row: D / 4 threads hold four columns each, and
+// 256 / (D / 4) of them share the splits, in a fixed order.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void q4_merge_kernel(Q4AttnArgs a) {
-  constexpr int kLanes = D / 4;
+  constexpr int kLanes = D / 4, kShares = 256 / kLanes;
+  __shared__ __attribute__((aligned(16))) float sums[kShares][D];
+  __shared__ float tops[kShares], zs[kShares];
   const Request rq = request_of(a, blockIdx.y);
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * (256 / kLanes) + threadIdx.x / kLanes;
-  if (i >= static_cast<int64_t>(rq.n) * a.n_q_heads) return;
+  const int64_t i = blockIdx.x;
+  if (i >= static_cast<int64_t>(rq.n) * a.n_q_heads) return;  // (the whole workgroup)
   const int64_t row = rq.first * a.n_q_heads + i;
-  const int d0 = threadIdx.x % kLanes * 4;
+  const int lane = threadIdx.x % kLanes, share = threadIdx.x / kLanes;
   const float* part = a.ws_lse + row * a.n_splits;
+  // every thread finds the greatest of its share's log-sum-exps; what is no number makes z no number
   float top = -INFINITY;
-  bool nan = false;
-  for (int s = 0; s < a.n_splits; ++s) {
-    top = fmaxf(top, part[s]);
-    nan |= part[s] != part[s];
-  }
+  for (int s = share; s < a.n_splits; s += kShares) top = fmaxf(top, part[s]);
   float z = 0.f;
   f32x4 o = f32x4{0};
-  if (top != -INFINITY)
-    for (int s = 0; s < a.n_splits; ++s) {
-      if (part[s] == -INFINITY) continue;
-      const float f = __builtin_amdgcn_exp2f(part[s] - top);
-      z += f;
-      o += *reinterpret_cast<const f32x4*>(a.ws_o + (row * a.n_splits + s) * D + d0) * f;
-    }
+#pragma unroll 4
+  for (int s = share; s < a.n_splits; s += kShares) {
+    const float lse = part[s];
+    if (lse == -INFINITY) continue;  // (its output is not written)
+    const float f = __builtin_amdgcn_exp2f(lse - (top == -INFINITY ? 0.f : top));
+    z += f;
+    o += *reinterpret_cast<const f32x4*>(a.ws_o + (row * a.n_splits + s) * D + 4 * lane) * f;
+  }
+  *reinterpret_cast<f32x4*>(&sums[share][4 * lane]) = o;
+  if (lane == 0) {
+    tops[share] = top;
+    zs[share] = z;
+  }
+  __syncthreads();
+  if (threadIdx.x >= kLanes) return;
+  top = tops[0];
+#pragma unroll
+  for (int k = 1; k < kShares; ++k) top = fmaxf(top, tops[k]);
+  z = 0.f;
+  o = f32x4{0};
+#pragma unroll
+  for (int k = 0; k < kShares; ++k) {
+    const float f = tops[k] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(tops[k] - top);
+    z = fmaf(f, zs[k], z);
+    o += *reinterpret_cast<const f32x4*>(&sums[k][4 * lane]) * f;
+  }
   const float inv = z == 0.f ? 0.f : 1.f / z;
-  o = nan ? f32x4{NAN, NAN, NAN, NAN} : o * inv;
   typedef T vec __attribute__((ext_vector_type(4)));
-  *reinterpret_cast<vec*>(a.out + (row * D + d0) * sizeof(T)) = __builtin_convertvector(o, vec);
-  if (a.lse && d0 == 0) a.lse[row] = nan ? NAN : z == 0.f ? -INFINITY : (top + log2f(z)) * 0.6931471805599453f;
+  *reinterpret_cast<vec*>(a.out + (row * D + 4 * lane) * sizeof(T)) = __builtin_convertvector(o * inv, vec);
+  if (a.lse && lane == 0) a.lse[row] = z == 0.f ? -INFINITY : (top == -INFINITY ? z : top + log2f(z)) * 0.6931471805599453f;
 }
 
-// How the keys are cut: into splits of whole units for every wavefront, so that the launch has some 1024 workgroups
-// (four a compute unit) where the requests alone do not supply them, but no less than two units a wavefront.
+// How the keys are cut: into splits of whole units for every wavefront, so that one round of workgroups covers the chip where
+// the requests alone do not, but no less than two units a wavefront.  Lengths differ, and a launch is over when its longest
+// split is: splits are cut down to 32 units as long as that makes no more than eight rounds of them.
 struct Cut {
   int32_t n_splits, split_units;
 };
 Cut cut_of(const mpic_ctx* ctx, int32_t n_requests, int32_t max_q, int64_t max_len) {
-  constexpr int64_t kWorkgroups = 1024, kLeast = 2 * kWaves;
+  constexpr int64_t kRound = 1024, kRounds = 8, kLeast = 2 * kWaves, kMost = 32;
   const int64_t units = std::max<int64_t>(1, (max_len + kUnit - 1) / kUnit);
   const int64_t tiles = (static_cast<int64_t>(max_q) * ctx->group + kCols - 1) / kCols;
   const int64_t lanes = tiles * ctx->cfg.n_kv_heads * n_requests;
-  const int64_t want = std::min(std::max<int64_t>(1, kWorkgroups / lanes), (units + kLeast - 1) / kLeast);
-  const int64_t each = ((units + want - 1) / want + kWaves - 1) / kWaves * kWaves;
+  const auto units_of = [&](int64_t workgroups) {  // a split's, for that many workgroups at most
+    const int64_t splits = std::max<int64_t>(1, workgroups / lanes);
+    return ((units + splits - 1) / splits + kWaves - 1) / kWaves * kWaves;
+  };
+  const int64_t each = std::max(kLeast, std::min(units_of(kRound), std::max(kMost, units_of(kRounds * kRound))));
   return Cut{static_cast<int32_t>((units + each - 1) / each), static_cast<int32_t>(each)};
 }
 bool sizes_fit(const mpic_ctx* ctx, int32_t n_requests, int64_t n_rows, int32_t max_q, int64_t max_len) {
@@ -441,10 +529,9 @@ int64_t workspace_of(const mpic_ctx* ctx, const Cut& cut, int64_t n_rows) {
 
 template <typename T, int D>
 void launch_q4_attn(const Q4AttnArgs& a, dim3 grid, int32_t n_requests, hipStream_t stream) {
-  hipLaunchKernelGGL((q4_attn_kernel<T, D>), grid, dim3(kWaves * 64), 0, stream, a);
+  hipLaunchKernelGGL((q4_attn_kernel<T, D>), grid, dim3(kWaves * 64), (AttnLds<T, D>::kBytes), stream, a);
   if (a.n_splits > 1) {
-    const int64_t rows = static_cast<int64_t>(a.max_q) * a.n_q_heads, each = 256 / (D / 4);
-    hipLaunchKernelGGL((q4_merge_kernel<T, D>), dim3(static_cast<unsigned>((rows + each - 1) / each), n_requests), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((q4_merge_kernel<T, D>), dim3(static_cast<unsigned>(a.max_q) * a.n_q_heads, n_requests), dim3(256), 0, stream, a);
   }
 }
 
