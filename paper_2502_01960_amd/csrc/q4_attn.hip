@@ -37,7 +37,6 @@ using q4::kTokens;
 
 constexpr int kWaves = 4;
 constexpr int kUnit = 32;       // tokens a wavefront takes at a time: two blocks
-constexpr int kCols = 16;       // flattened rows of a tile
 constexpr float kSlack = 8.0f;  // a column's reference point may lag behind its greatest score by this much, log2 units
 
 struct Q4AttnArgs {
@@ -88,7 +87,10 @@ __device__ inline uint32_t pair_of(uint32_t w) {
     return __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, hi), __builtin_bit_cast(uint32_t, lo), 0x07060302u);
   }
   const uint32_t moved = n == 0 ? w << 3 : w >> (4 * n - 3);
-  return (moved & 0x00780078u) | 0x3F803F80u;
+  // (one instruction, which takes a single constant from a scalar register: the mask stands in a vector register)
+  uint32_t r;
+  asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(r) : "v"(moved), "v"(0x00780078u), "s"(0x3F803F80u));
+  return r;
 }
 template <bool kExact>
 __device__ inline bf16x8 keys_of(uint32_t w) {
@@ -118,14 +120,25 @@ __device__ inline Parts<kParts> split_parts(f32x8 x) {
   return r;
 }
 
-template <typename T, int D>
+// How a wavefront's tiles of 16 columns are used.  Wide: a column is a row, and a lane works on all groups of its tokens.
+// Narrow (head_dim 128, up to eight rows): the eight rows stand in the columns twice, the lower eight columns work on the
+// first group of 64 values, the upper eight on the second.  A lane then reads, unpacks and applies the pairs of one group
+// only, and what it lacks of a score is in the lane eight further: 270 instead of 400 vector instructions a unit.
+template <typename T, int D, bool kNarrow_, int kTiles_>
 struct Shape {
+  using Type = T;
   using B = Block<T, D>;
+  static constexpr int kDim = D;
+  static constexpr bool kNarrow = kNarrow_;
+  static constexpr int kTiles = kTiles_;  // column tiles of a wavefront
   static constexpr bool kExact = std::is_same<T, float>::value;
   static constexpr int kParts = kExact ? 3 : 1;
   static constexpr int kGroups = B::kGroups;
+  static constexpr int kLaneGroups = kNarrow ? 1 : kGroups;  // groups a lane works on
+  static constexpr int kRows = kNarrow ? 8 : 16 * kTiles;    // flattened rows of a workgroup
   static constexpr int kWords = B::kLaneBytes / 4;
   static constexpr float kCode = kExact ? 1.f : 16.f;  // what a product with the codes has to be multiplied with
+  static_assert(!kNarrow || (kGroups == 2 && !kExact && kTiles == 1), "two groups share the columns");
 };
 
 // A unit in LDS: the codes of its two blocks (K, then V), then the pairs of the first block (K, V), then of the second
@@ -140,7 +153,7 @@ struct Unit {
 };
 template <typename T, int D>
 struct Held {
-  typedef uint32_t words __attribute__((ext_vector_type(Shape<T, D>::kWords)));
+  typedef uint32_t words __attribute__((ext_vector_type(Block<T, D>::kLaneBytes / 4)));
   typedef T pairs __attribute__((ext_vector_type(8)));  // scale, low of four tokens
 };
 // Block b's codes (kV: of V) and pairs of group g in this lane
@@ -158,12 +171,13 @@ __device__ inline typename Held<T, D>::pairs pairs_in(const char* unit, int b, i
 
 // Direct loads of 1024 and 2 x 1024 contiguous bytes to LDS, 16 a lane: base in scalar registers, the lane's offset in one
 // vector register (an instruction's offset moves both addresses).  No compiler-visible load: the wait is by hand.
+// Non-temporal: a decode step reads its contexts once (24 contexts, 442 MB: loads alone 107 -> 98 us).
 __device__ inline void stage_1k(const char* base, uint32_t offset, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(offset), "s"(base), "s"(lds) : "memory", "m0");
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt" : : "v"(offset), "s"(base), "s"(lds) : "memory", "m0");
 }
 __device__ inline void stage_2k(const char* base, uint32_t offset, uint32_t lds) {
   asm volatile(
-      "s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1\n\tglobal_load_lds_dwordx4 %0, %1 offset:1024"
+      "s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt\n\tglobal_load_lds_dwordx4 %0, %1 offset:1024 nt"
       :
       : "v"(offset), "s"(base), "s"(lds)
       : "memory", "m0");
@@ -185,173 +199,217 @@ __device__ inline void stage_unit(const char* block0, const char* block1, int la
 
 __device__ inline f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
+constexpr float kLowest = -3e38f;  // reference point of a column that has seen nothing
+
 // State of a column tile in one wavefront
-template <typename T, int D>
+template <typename S>
 struct Columns {
-  using S = Shape<T, D>;
-  Parts<S::kParts> q[S::kGroups][2];
-  float q_sum[S::kGroups];
-  f32x4 o[S::kGroups][4];  // O^T: lane (column, quarter g) holds columns 64 gr + 16 g + 4 r + tile of the output
-  f32x4 ones[S::kGroups];  // sums of the rounded weights
-  float low[S::kGroups];   // sum p * (low + 8 scale), F32: sum p * low; this lane's tokens
-  float m, l;              // reference point (log2 units, the same in the lanes of a column), sum p of this lane's tokens
-  int limit;               // positions 0 .. limit - 1 are seen
+  Parts<S::kParts> q[S::kGroups][2];  // (narrow: zeros where a column does not work on the group)
+  float q_sum[S::kLaneGroups];
+  f32x4 o[S::kGroups][4];      // O^T: lane (column, quarter c) holds columns 64 g + 16 c + 4 r + tile of the output
+  f32x4 ones[S::kLaneGroups];  // sums of the rounded weights
+  float low[S::kLaneGroups];   // sum p * (low + 8 scale), F32: sum p * low; this lane's tokens
+  float m, l;                  // reference point (log2 units, the same in the lanes of a column), sum p of this lane's tokens
+  int limit;                   // positions 0 .. limit - 1 are seen
 };
 
+// What the lane eight further among sixteen holds
+__device__ inline float other_half(float x) {
+  const int i = __builtin_bit_cast(int, x);
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(i, i, 0x128, 0xf, 0xf, true));  // rotation of the row by eight
+}
+
 // One unit of 32 tokens.  kMasked: not every token is seen by every column (or a block is missing: bit of `have`).
-template <typename T, int D, bool kMasked>
-__device__ inline void attend_unit(Columns<T, D>& s, const char* unit, int pos, int have, int lane, float factor) {
-  using S = Shape<T, D>;
-  const int quarter = lane >> 4;
-  float x[2][4];
+template <typename S, bool kMasked>
+__device__ inline void attend_unit(Columns<S> (&tiles)[S::kTiles], const char* unit, int pos, int have, int lane, float factor) {
+  using T = typename S::Type;
+  constexpr int D = S::kDim;
+  typedef typename Held<T, D>::words words;
+  typedef typename Held<T, D>::pairs pairs;
+  const int quarter = lane >> 4, my_group = S::kNarrow ? (lane >> 3 & 1) : 0;
 #pragma unroll
-  for (int b = 0; b < 2; ++b) {
-    f32x4 sum = f32x4{0};
-    const typename Held<T, D>::words words = codes_in<T, D, false>(unit, b, lane);
-#pragma unroll
-    for (int g = 0; g < S::kGroups; ++g) {
-      const typename Held<T, D>::pairs pairs = pairs_in<T, D, false>(unit, b, g, quarter);
-      const float start = S::kExact ? 0.f : -s.q_sum[g];
-      f32x4 acc = {start, start, start, start};
-#pragma unroll
-      for (int w = 0; w < 2; ++w) {
-        const bf16x8 codes = keys_of<S::kExact>(words[2 * g + w]);
-#pragma unroll
-        for (int i = 0; i < S::kParts; ++i) acc = mfma(codes, s.q[g][w].p[i], acc);
-      }
-      const float base = s.q_sum[g] * (1.f / S::kCode);
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-        sum[r] = fmaf(static_cast<float>(pairs[2 * r]), acc[r], fmaf(static_cast<float>(pairs[2 * r + 1]), base, sum[r]));
-    }
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const bool seen = !kMasked || ((have >> b & 1) && pos + kTokens * b + 4 * quarter + r < s.limit);
-      x[b][r] = seen ? sum[r] : -INFINITY;
-    }
-  }
-  float top = x[0][0];
-#pragma unroll
-  for (int i = 1; i < 8; ++i) top = fmaxf(top, x[i / 4][i % 4]);
-  top *= factor;
-  if (__any(top > s.m + kSlack)) {
-    float m = fmaxf(s.m, top);
-    m = fmaxf(m, __shfl_xor(m, 16));
-    m = fmaxf(m, __shfl_xor(m, 32));
-    const float f = m == -INFINITY ? 1.f : exp2f(s.m - m);
-    s.m = m;
-    s.l *= f;
-#pragma unroll
-    for (int g = 0; g < S::kGroups; ++g) {
-      s.low[g] *= f;
-      if (!S::kExact) s.ones[g] *= f;
-#pragma unroll
-      for (int c = 0; c < 4; ++c) s.o[g][c] *= f;
-    }
-  }
-  const float m = s.m == -INFINITY ? 0.f : s.m;
-  float p[2][4];
-#pragma unroll
-  for (int b = 0; b < 2; ++b)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      p[b][r] = __builtin_amdgcn_exp2f(fmaf(x[b][r], factor, -m));
-      s.l += p[b][r];
-    }
-  const typename Held<T, D>::words v0 = codes_in<T, D, true>(unit, 0, lane), v1 = codes_in<T, D, true>(unit, 1, lane);
-#pragma unroll
-  for (int g = 0; g < S::kGroups; ++g) {
-    f32x8 w;
+  for (int t = 0; t < S::kTiles; ++t) {
+    Columns<S>& s = tiles[t];
+    float x[2][4];
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-      const typename Held<T, D>::pairs pairs = pairs_in<T, D, true>(unit, b, g, quarter);
+      const words k = codes_in<T, D, false>(unit, b, lane);
+      f32x4 acc[S::kLaneGroups];
+#pragma unroll
+      for (int g = 0; g < S::kGroups; ++g) {
+        const int lg = S::kNarrow ? 0 : g;
+        if (!S::kNarrow || g == 0) {
+          const float start = S::kExact ? 0.f : -s.q_sum[lg];
+          acc[lg] = f32x4{start, start, start, start};
+        }
+        const bf16x8 keys[2] = {keys_of<S::kExact>(k[2 * g]), keys_of<S::kExact>(k[2 * g + 1])};
+        // (the small parts first)
+#pragma unroll
+        for (int i = S::kParts - 1; i >= 0; --i)
+#pragma unroll
+          for (int w = 0; w < 2; ++w) acc[lg] = mfma(keys[w], s.q[g][w].p[i], acc[lg]);
+      }
+      f32x4 sum = f32x4{0};
+#pragma unroll
+      for (int g = 0; g < S::kLaneGroups; ++g) {
+        const pairs p = pairs_in<T, D, false>(unit, b, S::kNarrow ? my_group : g, quarter);
+        const float base = s.q_sum[g] * (1.f / S::kCode);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float low = static_cast<float>(p[2 * r + 1]);
+          sum[r] = fmaf(static_cast<float>(p[2 * r]), acc[g][r], g ? fmaf(low, base, sum[r]) : low * base);
+        }
+      }
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        float scaled = p[b][r] * static_cast<float>(pairs[2 * r]);
-        float low = p[b][r] * static_cast<float>(pairs[2 * r + 1]);
-        if (kMasked && x[b][r] == -INFINITY) scaled = low = 0.f;  // (what is not seen may be no number)
-        w[4 * b + (r & 1) * 2 + (r >> 1)] = scaled;               // tokens (0, 2), (1, 3)
-        s.low[g] += S::kExact ? low : fmaf(8.f, scaled, low);
+        if (S::kNarrow) sum[r] += other_half(sum[r]);
+        const bool seen = !kMasked || ((have >> b & 1) && pos + kTokens * b + 4 * quarter + r < s.limit);
+        x[b][r] = seen ? sum[r] : -INFINITY;
       }
     }
-    const Parts<S::kParts> weights = split_parts<S::kParts>(w);
+    float top = x[0][0];
 #pragma unroll
-    for (int i = 0; i < S::kParts; ++i) {
-      if (!S::kExact) {
-        const u32x4 one = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
-        s.ones[g] = mfma(__builtin_bit_cast(bf16x8, one), weights.p[i], s.ones[g]);
+    for (int i = 1; i < 8; ++i) top = fmaxf(top, x[i / 4][i % 4]);
+    top *= factor;
+    if (__any(top > s.m + kSlack)) {
+      float m = fmaxf(s.m, top);
+      m = fmaxf(m, __shfl_xor(m, 16));
+      m = fmaxf(m, __shfl_xor(m, 32));
+      const float f = __builtin_amdgcn_exp2f(s.m - m);
+      s.m = m;
+      s.l *= f;
+#pragma unroll
+      for (int g = 0; g < S::kLaneGroups; ++g) {
+        s.low[g] *= f;
+        if (!S::kExact) s.ones[g] *= f;
       }
+#pragma unroll
+      for (int g = 0; g < S::kGroups; ++g)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) s.o[g][c] *= f;
+    }
+    float p[2][4];
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        p[b][r] = __builtin_amdgcn_exp2f(fmaf(x[b][r], factor, -s.m));
+        s.l += p[b][r];
+      }
+    Parts<S::kParts> weights[S::kLaneGroups];
+#pragma unroll
+    for (int g = 0; g < S::kLaneGroups; ++g) {
+      f32x8 w;
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const pairs vp = pairs_in<T, D, true>(unit, b, S::kNarrow ? my_group : g, quarter);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          float scaled = p[b][r] * static_cast<float>(vp[2 * r]);
+          float low = static_cast<float>(vp[2 * r + 1]);
+          if (kMasked && x[b][r] == -INFINITY) scaled = low = 0.f;  // (what is not seen may be no number)
+          w[4 * b + (r & 1) * 2 + (r >> 1)] = scaled;               // tokens (0, 2), (1, 3)
+          s.low[g] = fmaf(p[b][r], low, s.low[g]);
+          if (!S::kExact) s.low[g] = fmaf(8.f, scaled, s.low[g]);
+        }
+      }
+      weights[g] = split_parts<S::kParts>(w);
+    }
+    if (!S::kExact) {
+      const u32x4 one = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
+#pragma unroll
+      for (int g = 0; g < S::kLaneGroups; ++g) s.ones[g] = mfma(__builtin_bit_cast(bf16x8, one), weights[g].p[0], s.ones[g]);
+    }
+    const words v0 = codes_in<T, D, true>(unit, 0, lane), v1 = codes_in<T, D, true>(unit, 1, lane);
+#pragma unroll
+    for (int g = 0; g < S::kGroups; ++g)
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        s.o[g][2 * c] = mfma(values_of<S::kExact, 0>(v0[2 * g + c], v1[2 * g + c]), weights.p[i], s.o[g][2 * c]);
-        s.o[g][2 * c + 1] = mfma(values_of<S::kExact, 1>(v0[2 * g + c], v1[2 * g + c]), weights.p[i], s.o[g][2 * c + 1]);
+        const bf16x8 even = values_of<S::kExact, 0>(v0[2 * g + c], v1[2 * g + c]), odd = values_of<S::kExact, 1>(v0[2 * g + c], v1[2 * g + c]);
+#pragma unroll
+        for (int i = S::kParts - 1; i >= 0; --i) {
+          s.o[g][2 * c] = mfma(even, weights[S::kNarrow ? 0 : g].p[i], s.o[g][2 * c]);
+          s.o[g][2 * c + 1] = mfma(odd, weights[S::kNarrow ? 0 : g].p[i], s.o[g][2 * c + 1]);
+        }
       }
-    }
   }
 }
 
-// LDS: the units of every wavefront; at the end their partial results (rows of D + 4 floats, reference points, sums)
-template <typename T, int D>
+// LDS: the units of every wavefront; at the end their partial results of a tile (rows of D + 4 floats, reference points, sums)
+template <typename S>
 struct AttnLds {
-  static constexpr int kRow = D + 4;
-  static constexpr int kWave = 2 * Unit<T, D>::kBytes;
-  static constexpr int kParts = kWaves * kCols * (kRow + 2) * 4;
-  static constexpr int kBytes = kWaves * kWave > kParts ? kWaves * kWave : kParts;
+  using U = Unit<typename S::Type, S::kDim>;
+  static constexpr int kRow = S::kDim + 4;
+  static constexpr int kCols = S::kNarrow ? 8 : 16;  // rows of a tile
+  static constexpr int kWave = 2 * U::kBytes;
+  static constexpr int kMerge = kWaves * kCols * (kRow + 2) * 4;
+  static constexpr int kBytes = kWaves * kWave > kMerge ? kWaves * kWave : kMerge;
   static_assert(kBytes <= 65536, "no opt-in needed");
 };
 
-template <typename T, int D>
-__global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 3 : 2) void q4_attn_kernel(Q4AttnArgs a) {
-  using S = Shape<T, D>;
+template <typename S, int kWavesPerSimd>
+__global__ __launch_bounds__(kWaves * 64, kWavesPerSimd) void q4_attn_kernel(Q4AttnArgs a) {
+  using T = typename S::Type;
+  constexpr int D = S::kDim;
   using B = Block<T, D>;
-  using L = AttnLds<T, D>;
+  using L = AttnLds<S>;
   using U = Unit<T, D>;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
-  typedef float PartRows[kCols][L::kRow];
-  typedef float PartCols[kCols];
+  typedef float PartRows[L::kCols][L::kRow];
+  typedef float PartCols[L::kCols];
   PartRows* part_o = reinterpret_cast<PartRows*>(lds);
   PartCols* part_m = reinterpret_cast<PartCols*>(part_o + kWaves);
   PartCols* part_l = part_m + kWaves;
-  const int lane = threadIdx.x & 63, col = lane & 15, quarter = lane >> 4;
+  const int lane = threadIdx.x & 63, col = lane & (L::kCols - 1), quarter = lane >> 4;
+  const int my_group = S::kNarrow ? (lane >> 3 & 1) : 0;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int split = blockIdx.x, head = blockIdx.y % a.n_kv_heads, b = blockIdx.z;
-  const int row0 = static_cast<int>(blockIdx.y) / a.n_kv_heads * kCols;
+  // heads first: neighbouring workgroups go to different L2 domains, which thus get the same share of every split, and the
+  // row tiles of a head that read the same keys run together
+  const int head = blockIdx.x % a.n_kv_heads, split = blockIdx.y, b = blockIdx.z;
+  const int row0 = static_cast<int>(blockIdx.x / a.n_kv_heads) * S::kRows;
   const Request rq = request_of(a, b);
   const int n_flat = rq.n * a.group;
   if (row0 >= n_flat) return;
-  const int last = (min(row0 + kCols, n_flat) - 1) / a.group;  // last query of the tile
+  const int last = (min(row0 + S::kRows, n_flat) - 1) / a.group;  // last query of the workgroup
   const int behind = rq.len - rq.n;                            // tokens in front of the new ones (negative: some have no position)
   const int key_end = max(behind + last + 1, 0);
   const int key_all = behind + row0 / a.group + 1;             // the keys below are seen by every row
+  const int unit_end = min((key_end + kUnit - 1) / kUnit, (split + 1) * a.split_units);
+  if (a.n_splits > 1 && unit_end <= split * a.split_units) return;  // (the merge asks for no such split)
 
-  Columns<T, D> s;
-  const int flat = min(row0 + col, n_flat - 1), token = flat / a.group, hq = head * a.group + flat % a.group;
-  s.limit = row0 + col < n_flat ? behind + token + 1 : 0;
-  s.m = -INFINITY;
-  s.l = 0.f;
-  {
+  Columns<S> tiles[S::kTiles];
+#pragma unroll
+  for (int t = 0; t < S::kTiles; ++t) {
+    Columns<S>& s = tiles[t];
+    const int at = row0 + 16 * t + col, flat = min(at, n_flat - 1), token = flat / a.group, hq = head * a.group + flat % a.group;
+    s.limit = at < n_flat ? behind + token + 1 : 0;
+    s.m = kLowest;
+    s.l = 0.f;
     const char* q = a.q + (rq.first + token) * a.q_stride + static_cast<int64_t>(hq) * D * sizeof(T);
 #pragma unroll
+    for (int g = 0; g < S::kLaneGroups; ++g) s.q_sum[g] = s.low[g] = 0.f, s.ones[g] = f32x4{0};
+#pragma unroll
     for (int g = 0; g < S::kGroups; ++g) {
-      s.q_sum[g] = 0.f;
-      s.low[g] = 0.f;
-      s.ones[g] = f32x4{0};
+      const int lg = S::kNarrow ? 0 : g;
 #pragma unroll
       for (int c = 0; c < 4; ++c) s.o[g][c] = f32x4{0};
 #pragma unroll
       for (int w = 0; w < 2; ++w) {
         typedef T vec __attribute__((ext_vector_type(8), aligned(16)));
         f32x8 x = __builtin_convertvector(*reinterpret_cast<const vec*>(q + (g * q4::kGroup + quarter * 16 + w * 8) * sizeof(T)), f32x8);
+        if (S::kNarrow && g != my_group) x = f32x8{0};
         s.q[g][w] = split_parts<S::kParts>(x);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s.q_sum[g] += x[e];
+        for (int e = 0; e < 8; ++e) s.q_sum[lg] += x[e];
       }
+    }
+#pragma unroll
+    for (int g = 0; g < S::kLaneGroups; ++g) {
       s.q_sum[g] += __shfl_xor(s.q_sum[g], 16);
       s.q_sum[g] += __shfl_xor(s.q_sum[g], 32);
     }
   }
   const float factor = a.scale_log2 * S::kCode;
-  const int unit_end = min((key_end + kUnit - 1) / kUnit, (split + 1) * a.split_units);
   const int unit0 = split * a.split_units + wave;
   const int n_units = unit_end > unit0 ? (unit_end - unit0 + kWaves - 1) / kWaves : 0;  // of this wavefront
   const int32_t* table = a.table + b * a.table_width;
@@ -390,65 +448,70 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 3 : 2) void q4_attn_k
     const char* unit = ring + (i & 1) * U::kBytes;
     const int pos = (unit0 + i * kWaves) * kUnit;
     if (have == 3 && pos + kUnit <= key_all)
-      attend_unit<T, D, false>(s, unit, pos, have, lane, factor);
+      attend_unit<S, false>(tiles, unit, pos, have, lane, factor);
     else
-      attend_unit<T, D, true>(s, unit, pos, have, lane, factor);
+      attend_unit<S, true>(tiles, unit, pos, have, lane, factor);
     have = have_next;
   }
-  __syncthreads();
 
-  s.l += __shfl_xor(s.l, 16);
-  s.l += __shfl_xor(s.l, 32);
-  if (quarter == 0) {
-    part_m[wave][col] = s.m;
-    part_l[wave][col] = s.l;
-  }
 #pragma unroll
-  for (int g = 0; g < S::kGroups; ++g) {
-    s.low[g] += __shfl_xor(s.low[g], 16);
-    s.low[g] += __shfl_xor(s.low[g], 32);
+  for (int t = 0; t < S::kTiles; ++t) {
+    Columns<S>& s = tiles[t];
+    __syncthreads();  // (the ring, or the tile before, has been read)
+    s.l += __shfl_xor(s.l, 16);
+    s.l += __shfl_xor(s.l, 32);
+    if (lane < L::kCols) {
+      part_m[wave][col] = s.m;
+      part_l[wave][col] = s.l;
+    }
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      f32x4 o;
+    for (int g = 0; g < S::kLaneGroups; ++g) {
+      s.low[g] += __shfl_xor(s.low[g], 16);
+      s.low[g] += __shfl_xor(s.low[g], 32);
+      const int group = S::kNarrow ? my_group : g;
 #pragma unroll
-      for (int c = 0; c < 4; ++c) o[c] = S::kExact ? s.o[g][c][r] + s.low[g] : fmaf(fmaf(-1.5f, s.ones[g][r], s.o[g][c][r]), S::kCode, s.low[g]);
-      *reinterpret_cast<f32x4*>(&part_o[wave][col][g * q4::kGroup + quarter * 16 + 4 * r]) = o;
+      for (int r = 0; r < 4; ++r) {
+        f32x4 o;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const float sum = S::kNarrow && my_group ? s.o[S::kGroups - 1][c][r] : s.o[g][c][r];
+          o[c] = S::kExact ? sum + s.low[g] : fmaf(fmaf(-1.5f, s.ones[g][r], sum), S::kCode, s.low[g]);
+        }
+        *reinterpret_cast<f32x4*>(&part_o[wave][col][group * q4::kGroup + quarter * 16 + 4 * r]) = o;
+      }
+    }
+    __syncthreads();
+
+    constexpr int kThreads = kWaves * 64 / L::kCols, kEach = D / kThreads;  // threads and values per row
+    typedef float each __attribute__((ext_vector_type(kEach)));
+    const int c = threadIdx.x / kThreads, d0 = threadIdx.x % kThreads * kEach, at = row0 + 16 * t + c;
+    if (at < n_flat) {
+      float top = part_m[0][c];
+#pragma unroll
+      for (int w = 1; w < kWaves; ++w) top = fmaxf(top, part_m[w][c]);
+      float z = 0.f;
+      each o = each{0};
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const float f = __builtin_amdgcn_exp2f(part_m[w][c] - top);
+        z = fmaf(f, part_l[w][c], z);
+        o += *reinterpret_cast<const each*>(&part_o[w][c][d0]) * f;
+      }
+      const bool none = z == 0.f;
+      const float inv = none ? 0.f : 1.f / z, lse2 = none ? -INFINITY : top + log2f(z);
+      o *= inv;
+      const int64_t row = (rq.first + at / a.group) * a.n_q_heads + head * a.group + at % a.group;
+      if (a.n_splits > 1) {
+        const int64_t part = row * a.n_splits + split;
+        if (d0 == 0) a.ws_lse[part] = lse2;
+        if (!none) *reinterpret_cast<each*>(a.ws_o + part * D + d0) = o;
+      } else {
+        typedef T vec __attribute__((ext_vector_type(kEach)));
+        *reinterpret_cast<vec*>(a.out + (row * D + d0) * sizeof(T)) = __builtin_convertvector(o, vec);
+        if (a.lse && d0 == 0) a.lse[row] = lse2 * 0.6931471805599453f;
+      }
     }
   }
-  __syncthreads();
-
-  constexpr int kEach = D / 16;  // values of a row per thread
-  const int c = threadIdx.x / 16, d0 = threadIdx.x % 16 * kEach;
-  if (row0 + c >= n_flat) return;
-  float top = part_m[0][c];
-#pragma unroll
-  for (int w = 1; w < kWaves; ++w) top = fmaxf(top, part_m[w][c]);
-  float z = 0.f, o[kEach] = {};
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    // (a wavefront that saw nothing, or nothing but what is no number, adds its sums as they are)
-    const float f = part_m[w][c] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(part_m[w][c] - top);
-    z = fmaf(f, part_l[w][c], z);
-#pragma unroll
-    for (int e = 0; e < kEach; ++e) o[e] = fmaf(f, part_o[w][c][d0 + e], o[e]);
-  }
-  const bool none = z == 0.f;
-  const float inv = none ? 0.f : 1.f / z, lse2 = none ? -INFINITY : (top == -INFINITY ? z : top + log2f(z));
-  const int64_t row = (rq.first + (row0 + c) / a.group) * a.n_q_heads + head * a.group + (row0 + c) % a.group;
-  if (a.n_splits > 1) {
-    const int64_t at = row * a.n_splits + split;
-    if (threadIdx.x % 16 == 0) a.ws_lse[at] = lse2;
-    if (!none)
-#pragma unroll
-      for (int e = 0; e < kEach; e += 4) *reinterpret_cast<f32x4*>(a.ws_o + at * D + d0 + e) = f32x4{o[e] * inv, o[e + 1] * inv, o[e + 2] * inv, o[e + 3] * inv};
-    return;
-  }
-  typedef T vec __attribute__((ext_vector_type(4)));
-#pragma unroll
-  for (int e = 0; e < kEach; e += 4)
-    *reinterpret_cast<vec*>(a.out + (row * D + d0 + e) * sizeof(T)) =
-        __builtin_convertvector((f32x4{o[e] * inv, o[e + 1] * inv, o[e + 2] * inv, o[e + 3] * inv}), vec);
-  if (a.lse && threadIdx.x % 16 == 0) a.lse[row] = lse2 * 0.6931471805599453f;
 }
 
 // Output rows from the partial results of their splits.  A workgroup takes a row: D / 4 threads hold four columns each, and
@@ -464,16 +527,19 @@ __global__ __launch_bounds__(256) void q4_merge_kernel(Q4AttnArgs a) {
   const int64_t row = rq.first * a.n_q_heads + i;
   const int lane = threadIdx.x % kLanes, share = threadIdx.x / kLanes;
   const float* part = a.ws_lse + row * a.n_splits;
+  // splits that hold keys of this row
+  const int keys = max(rq.len - rq.n + static_cast<int>(i) / a.n_q_heads + 1, 0);
+  const int n_splits = keys > 0 ? min((keys - 1) / (kUnit * a.split_units) + 1, a.n_splits) : 0;
   // every thread finds the greatest of its share's log-sum-exps; what is no number makes z no number
-  float top = -INFINITY;
-  for (int s = share; s < a.n_splits; s += kShares) top = fmaxf(top, part[s]);
+  float top = kLowest;
+  for (int s = share; s < n_splits; s += kShares) top = fmaxf(top, part[s]);
   float z = 0.f;
   f32x4 o = f32x4{0};
 #pragma unroll 4
-  for (int s = share; s < a.n_splits; s += kShares) {
+  for (int s = share; s < n_splits; s += kShares) {
     const float lse = part[s];
     if (lse == -INFINITY) continue;  // (its output is not written)
-    const float f = __builtin_amdgcn_exp2f(lse - (top == -INFINITY ? 0.f : top));
+    const float f = __builtin_amdgcn_exp2f(lse - top);
     z += f;
     o += *reinterpret_cast<const f32x4*>(a.ws_o + (row * a.n_splits + s) * D + 4 * lane) * f;
   }
@@ -491,48 +557,58 @@ __global__ __launch_bounds__(256) void q4_merge_kernel(Q4AttnArgs a) {
   o = f32x4{0};
 #pragma unroll
   for (int k = 0; k < kShares; ++k) {
-    const float f = tops[k] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(tops[k] - top);
+    const float f = __builtin_amdgcn_exp2f(tops[k] - top);
     z = fmaf(f, zs[k], z);
     o += *reinterpret_cast<const f32x4*>(&sums[k][4 * lane]) * f;
   }
   const float inv = z == 0.f ? 0.f : 1.f / z;
   typedef T vec __attribute__((ext_vector_type(4)));
   *reinterpret_cast<vec*>(a.out + (row * D + 4 * lane) * sizeof(T)) = __builtin_convertvector(o * inv, vec);
-  if (a.lse && lane == 0) a.lse[row] = z == 0.f ? -INFINITY : (top == -INFINITY ? z : top + log2f(z)) * 0.6931471805599453f;
+  if (a.lse && lane == 0) a.lse[row] = z == 0.f ? -INFINITY : (top + log2f(z)) * 0.6931471805599453f;
 }
 
-// How the keys are cut: into splits of whole units for every wavefront, so that one round of workgroups covers the chip where
+// How the keys are cut: into splits of whole units for every wavefront, so that one round of workgroups (three a compute unit) covers the chip where
 // the requests alone do not, but no less than two units a wavefront.  Lengths differ, and a launch is over when its longest
 // split is: splits are cut down to 32 units as long as that makes no more than eight rounds of them.
 struct Cut {
+  int32_t rows;  // flattened rows of a workgroup
   int32_t n_splits, split_units;
+  int64_t tiles;
 };
+int32_t rows_of(const mpic_ctx* ctx, int32_t max_q) {
+  const int64_t flat = static_cast<int64_t>(max_q) * ctx->group;
+  return ctx->cfg.dtype == MPIC_BF16 && flat <= 8 ? 8 : 16;
+}
 Cut cut_of(const mpic_ctx* ctx, int32_t n_requests, int32_t max_q, int64_t max_len) {
-  constexpr int64_t kRound = 1024, kRounds = 8, kLeast = 2 * kWaves, kMost = 32;
+  constexpr int64_t kRound = 768, kRounds = 8, kLeast = 2 * kWaves, kMost = 32;
   const int64_t units = std::max<int64_t>(1, (max_len + kUnit - 1) / kUnit);
-  const int64_t tiles = (static_cast<int64_t>(max_q) * ctx->group + kCols - 1) / kCols;
-  const int64_t lanes = tiles * ctx->cfg.n_kv_heads * n_requests;
+  Cut cut;
+  cut.rows = rows_of(ctx, max_q);
+  cut.tiles = (static_cast<int64_t>(max_q) * ctx->group + cut.rows - 1) / cut.rows;
+  const int64_t lanes = cut.tiles * ctx->cfg.n_kv_heads * n_requests;
   const auto units_of = [&](int64_t workgroups) {  // a split's, for that many workgroups at most
     const int64_t splits = std::max<int64_t>(1, workgroups / lanes);
     return ((units + splits - 1) / splits + kWaves - 1) / kWaves * kWaves;
   };
   const int64_t each = std::max(kLeast, std::min(units_of(kRound), std::max(kMost, units_of(kRounds * kRound))));
-  return Cut{static_cast<int32_t>((units + each - 1) / each), static_cast<int32_t>(each)};
+  cut.split_units = static_cast<int32_t>(each);
+  cut.n_splits = static_cast<int32_t>((units + each - 1) / each);
+  return cut;
 }
 bool sizes_fit(const mpic_ctx* ctx, int32_t n_requests, int64_t n_rows, int32_t max_q, int64_t max_len) {
   return n_requests >= 0 && n_rows >= 0 && max_q >= 1 && max_len >= 0 && n_rows < INT32_MAX && max_len <= INT32_MAX - 64 &&
-         static_cast<int64_t>(max_q) * ctx->group < INT32_MAX - kCols;
+         static_cast<int64_t>(max_q) * ctx->group < INT32_MAX - 256;
 }
 int64_t workspace_of(const mpic_ctx* ctx, const Cut& cut, int64_t n_rows) {
   return cut.n_splits > 1 ? n_rows * ctx->cfg.n_q_heads * cut.n_splits * (ctx->cfg.head_dim + 1) * 4 : 0;
 }
 
-template <typename T, int D>
-void launch_q4_attn(const Q4AttnArgs& a, dim3 grid, int32_t n_requests, hipStream_t stream) {
-  hipLaunchKernelGGL((q4_attn_kernel<T, D>), grid, dim3(kWaves * 64), (AttnLds<T, D>::kBytes), stream, a);
-  if (a.n_splits > 1) {
-    hipLaunchKernelGGL((q4_merge_kernel<T, D>), dim3(static_cast<unsigned>(a.max_q) * a.n_q_heads, n_requests), dim3(256), 0, stream, a);
-  }
+template <typename S, int kWavesPerSimd>
+void launch_q4_attn(const Q4AttnArgs& a, dim3 grid, hipStream_t stream) {
+  hipLaunchKernelGGL((q4_attn_kernel<S, kWavesPerSimd>), grid, dim3(kWaves * 64), AttnLds<S>::kBytes, stream, a);
+  if (a.n_splits > 1)
+    hipLaunchKernelGGL((q4_merge_kernel<typename S::Type, S::kDim>), dim3(static_cast<unsigned>(a.max_q) * a.n_q_heads, grid.z), dim3(256), 0,
+                       stream, a);
 }
 
 }  // namespace
@@ -570,8 +646,7 @@ extern "C" int mpic_q4_attn(mpic_ctx* ctx, const void* q, int64_t q_stride, int6
     return invalid("q4_attn: buffers must be 16-byte aligned");
   const Cut cut = cut_of(ctx, n_requests, max_q, max_len);
   if (workspace_of(ctx, cut, n_rows) > (workspace ? workspace_bytes : 0)) return invalid("q4_attn: workspace too small");
-  const int64_t tiles = (static_cast<int64_t>(max_q) * ctx->group + kCols - 1) / kCols;
-  if (tiles * c.n_kv_heads > 65535 || n_requests > 65535)
+  if (cut.tiles * c.n_kv_heads > INT32_MAX / (kWaves * 64) || static_cast<int64_t>(max_q) * c.n_q_heads > INT32_MAX / 256 || n_requests > 65535)
     return fail(ctx, MPIC_ERR_UNSUPPORTED, "q4_attn: too many queries, heads or requests for one launch");
   const int rc = bind_device(ctx);
   if (rc != MPIC_OK) return rc;
@@ -599,13 +674,15 @@ extern "C" int mpic_q4_attn(mpic_ctx* ctx, const void* q, int64_t q_stride, int6
   a.group = ctx->group;
   a.scale_log2 = static_cast<float>(softmax_scale * 1.4426950408889634);
   hipStream_t stream = static_cast<hipStream_t>(stream_);
-  const dim3 grid(cut.n_splits, static_cast<unsigned>(tiles * c.n_kv_heads), n_requests);
-  if (c.dtype == MPIC_BF16)
-    launch_q4_attn<__bf16, 128>(a, grid, n_requests, stream);
+  const dim3 grid(static_cast<unsigned>(cut.tiles * c.n_kv_heads), cut.n_splits, n_requests);
+  if (c.dtype == MPIC_BF16 && cut.rows == 8)
+    launch_q4_attn<Shape<__bf16, 128, true, 1>, 3>(a, grid, stream);
+  else if (c.dtype == MPIC_BF16)
+    launch_q4_attn<Shape<__bf16, 128, false, 1>, 3>(a, grid, stream);
   else if (c.head_dim == 128)
-    launch_q4_attn<float, 128>(a, grid, n_requests, stream);
+    launch_q4_attn<Shape<float, 128, false, 1>, 2>(a, grid, stream);
   else
-    launch_q4_attn<float, 64>(a, grid, n_requests, stream);
+    launch_q4_attn<Shape<float, 64, false, 1>, 3>(a, grid, stream);
   MPIC_HIP(ctx, hipGetLastError());
   return MPIC_OK;
 }

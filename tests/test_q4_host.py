@@ -105,7 +105,7 @@ def test_attention_refuses(ctx):
     assert "q4_attn" in mpic.binding.mpic_last_error(ctx.handle)
     assert _attn(ctx, n_rows=0, n_requests=0) == 0
     assert _attn(ctx, n_rows=0, q_off=A, q=None, out=None) == 0
-    assert _attn(ctx, q_off=A, max_q=1 << 20) == UNSUPPORTED
+    assert _attn(ctx, q_off=A, max_q=1 << 21) == UNSUPPORTED
     assert _attn(ctx, n_rows=70000, n_requests=70000) == UNSUPPORTED
 
 
