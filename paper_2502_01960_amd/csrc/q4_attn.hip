@@ -367,6 +367,17 @@ __global__ __launch_bounds__(kWaves * 64, kWavesPerSimd) void q4_attn_kernel(Q4A
   // row tiles of a head that read the same keys run together
   const int head = blockIdx.x % a.n_kv_heads, split = blockIdx.y, b = blockIdx.z;
   const int row0 = static_cast<int>(blockIdx.x / a.n_kv_heads) * S::kRows;
+  // The way to the first keys is a chain of loads: what the table says of this wavefront's blocks is asked for before the
+  // length is known, and the first unit before the queries are converted.
+  const int unit0 = split * a.split_units + wave;
+  const int32_t* table = a.table + b * a.table_width;
+  // entry of the block that a lane looks after, two lanes a unit, from the wavefront's unit i0 on
+  const auto block_of_lane = [&](int i0) { return 2 * (unit0 + (i0 + (lane >> 1)) * kWaves) + (lane & 1); };
+  const auto entry_of = [&](int block) {
+    const int page = block / a.page_blocks;
+    return page < a.table_width ? table[page] : -1;
+  };
+  int entry = entry_of(block_of_lane(0));
   const Request rq = request_of(a, b);
   const int n_flat = rq.n * a.group;
   if (row0 >= n_flat) return;
@@ -378,50 +389,26 @@ __global__ __launch_bounds__(kWaves * 64, kWavesPerSimd) void q4_attn_kernel(Q4A
   if (a.n_splits > 1 && unit_end <= split * a.split_units) return;  // (the merge asks for no such split)
 
   Columns<S> tiles[S::kTiles];
+  typedef T vec __attribute__((ext_vector_type(8), aligned(16)));
+  vec raw[S::kTiles][S::kGroups][2];
 #pragma unroll
   for (int t = 0; t < S::kTiles; ++t) {
-    Columns<S>& s = tiles[t];
     const int at = row0 + 16 * t + col, flat = min(at, n_flat - 1), token = flat / a.group, hq = head * a.group + flat % a.group;
-    s.limit = at < n_flat ? behind + token + 1 : 0;
-    s.m = kLowest;
-    s.l = 0.f;
+    tiles[t].limit = at < n_flat ? behind + token + 1 : 0;
     const char* q = a.q + (rq.first + token) * a.q_stride + static_cast<int64_t>(hq) * D * sizeof(T);
 #pragma unroll
-    for (int g = 0; g < S::kLaneGroups; ++g) s.q_sum[g] = s.low[g] = 0.f, s.ones[g] = f32x4{0};
+    for (int g = 0; g < S::kGroups; ++g)
 #pragma unroll
-    for (int g = 0; g < S::kGroups; ++g) {
-      const int lg = S::kNarrow ? 0 : g;
-#pragma unroll
-      for (int c = 0; c < 4; ++c) s.o[g][c] = f32x4{0};
-#pragma unroll
-      for (int w = 0; w < 2; ++w) {
-        typedef T vec __attribute__((ext_vector_type(8), aligned(16)));
-        f32x8 x = __builtin_convertvector(*reinterpret_cast<const vec*>(q + (g * q4::kGroup + quarter * 16 + w * 8) * sizeof(T)), f32x8);
-        if (S::kNarrow && g != my_group) x = f32x8{0};
-        s.q[g][w] = split_parts<S::kParts>(x);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) s.q_sum[lg] += x[e];
-      }
-    }
-#pragma unroll
-    for (int g = 0; g < S::kLaneGroups; ++g) {
-      s.q_sum[g] += __shfl_xor(s.q_sum[g], 16);
-      s.q_sum[g] += __shfl_xor(s.q_sum[g], 32);
-    }
+      for (int w = 0; w < 2; ++w) raw[t][g][w] = *reinterpret_cast<const vec*>(q + (g * q4::kGroup + quarter * 16 + w * 8) * sizeof(T));
   }
-  const float factor = a.scale_log2 * S::kCode;
-  const int unit0 = split * a.split_units + wave;
   const int n_units = unit_end > unit0 ? (unit_end - unit0 + kWaves - 1) / kWaves : 0;  // of this wavefront
-  const int32_t* table = a.table + b * a.table_width;
-  // blocks of the next 32 units, two lanes a unit; -1: not in the cache
+  // the blocks of the next 32 units, two lanes a unit; -1: not in the cache
   int ids = -1;
-  auto look_up = [&](int i0) {
-    const int block = 2 * (unit0 + (i0 + (lane >> 1)) * kWaves) + (lane & 1);
-    ids = -1;
-    if (block < (key_end + kTokens - 1) / kTokens) {
-      const int64_t id = static_cast<int64_t>(table[block / a.page_blocks]) * a.page_blocks + block % a.page_blocks;
-      if (id >= 0 && id < a.n_blocks) ids = static_cast<int>(id);
-    }
+  const auto look_up = [&](int i0) {
+    const int block = block_of_lane(i0);
+    if (i0) entry = entry_of(block);
+    const int64_t id = static_cast<int64_t>(entry) * a.page_blocks + block % a.page_blocks;
+    ids = id >= 0 && id < a.n_blocks && block < (key_end + kTokens - 1) / kTokens ? static_cast<int>(id) : -1;
   };
   char* ring = lds + wave * L::kWave;
   const uint32_t ring_lds = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(MPIC_LDS_PTR(char, ring)));
@@ -436,6 +423,34 @@ __global__ __launch_bounds__(kWaves * 64, kWavesPerSimd) void q4_attn_kernel(Q4A
   };
   int have = 0;
   if (n_units > 0) have = stage(0);
+#pragma unroll
+  for (int t = 0; t < S::kTiles; ++t) {
+    Columns<S>& s = tiles[t];
+    s.m = kLowest;
+    s.l = 0.f;
+#pragma unroll
+    for (int g = 0; g < S::kLaneGroups; ++g) s.q_sum[g] = s.low[g] = 0.f, s.ones[g] = f32x4{0};
+#pragma unroll
+    for (int g = 0; g < S::kGroups; ++g) {
+      const int lg = S::kNarrow ? 0 : g;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) s.o[g][c] = f32x4{0};
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        f32x8 x = __builtin_convertvector(raw[t][g][w], f32x8);
+        if (S::kNarrow && g != my_group) x = f32x8{0};
+        s.q[g][w] = split_parts<S::kParts>(x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s.q_sum[lg] += x[e];
+      }
+    }
+#pragma unroll
+    for (int g = 0; g < S::kLaneGroups; ++g) {
+      s.q_sum[g] += __shfl_xor(s.q_sum[g], 16);
+      s.q_sum[g] += __shfl_xor(s.q_sum[g], 32);
+    }
+  }
+  const float factor = a.scale_log2 * S::kCode;
   for (int i = 0; i < n_units; ++i) {
     int have_next = 0;
     if (i + 1 < n_units) {
@@ -530,18 +545,34 @@ __global__ __launch_bounds__(256) void q4_merge_kernel(Q4AttnArgs a) {
   // splits that hold keys of this row
   const int keys = max(rq.len - rq.n + static_cast<int>(i) / a.n_q_heads + 1, 0);
   const int n_splits = keys > 0 ? min((keys - 1) / (kUnit * a.split_units) + 1, a.n_splits) : 0;
-  // every thread finds the greatest of its share's log-sum-exps; what is no number makes z no number
-  float top = kLowest;
-  for (int s = share; s < n_splits; s += kShares) top = fmaxf(top, part[s]);
-  float z = 0.f;
+  // eight splits at a time: their loads do not wait for each other, nor an output for the log-sum-exp that says whether it
+  // was written at all
+  constexpr int kBatch = 8;
+  float top = kLowest, z = 0.f;
   f32x4 o = f32x4{0};
-#pragma unroll 4
-  for (int s = share; s < n_splits; s += kShares) {
-    const float lse = part[s];
-    if (lse == -INFINITY) continue;  // (its output is not written)
-    const float f = __builtin_amdgcn_exp2f(lse - top);
-    z += f;
-    o += *reinterpret_cast<const f32x4*>(a.ws_o + (row * a.n_splits + s) * D + 4 * lane) * f;
+  for (int s0 = share; s0 < n_splits; s0 += kBatch * kShares) {
+    float lse[kBatch];
+    f32x4 part_o[kBatch];
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      const int s = s0 + k * kShares, at = min(s, n_splits - 1);
+      lse[k] = s < n_splits ? part[at] : -INFINITY;
+      part_o[k] = *reinterpret_cast<const f32x4*>(a.ws_o + (row * a.n_splits + at) * D + 4 * lane);
+    }
+    float m = top;
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) m = fmaxf(m, lse[k]);
+    const float f = __builtin_amdgcn_exp2f(top - m);
+    top = m;
+    z *= f;
+    o *= f;
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      const float w = __builtin_amdgcn_exp2f(lse[k] - m);
+      z += w;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = lse[k] == -INFINITY ? o[e] : fmaf(part_o[k][e], w, o[e]);
+    }
   }
   *reinterpret_cast<f32x4*>(&sums[share][4 * lane]) = o;
   if (lane == 0) {
@@ -662,7 +693,7 @@ extern "C" int mpic_q4_attn(mpic_ctx* ctx, const void* q, int64_t q_stride, int6
   a.ws_lse = a.ws_o + n_rows * c.n_q_heads * cut.n_splits * c.head_dim;
   a.n_rows = n_rows;
   a.q_stride = q_stride * elem;
-  a.table_width = table_width;
+  a.table_width = max_len > 0 ? table_width : 0;  // (there may be no table then)
   a.n_blocks = static_cast<int32_t>((n_slots + q4::kTokens - 1) / q4::kTokens);
   a.page_blocks = page_size / q4::kTokens;
   a.max_q = max_q;
