@@ -79,17 +79,20 @@ int mpic_q4_bytes(const mpic_ctx* ctx, int64_t n_slots, int64_t* bytes);
  *                     left out (padding).  A slot must not be named twice in a call: its content
  *                     is then undefined (part of one row, part of another)
  *   cache             device, 16-byte aligned; other slots keep what they hold
+ *   cache_bytes       size of the buffer, at least mpic_q4_bytes for n_slots
  * Errors: MPIC_ERR_INVALID, MPIC_ERR_HIP.
  */
 int mpic_q4_write(mpic_ctx* ctx, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
-                  int64_t n_rows, const int32_t* slots, void* cache, int64_t n_slots, void* stream);
+                  int64_t n_rows, const int32_t* slots, void* cache, int64_t cache_bytes, int64_t n_slots,
+                  void* stream);
 
 /*
  * Read rows back: k and v row r = the values that slot slots[r] holds.  Same arguments; a row
  * whose slot is not in 0 .. n_slots - 1 is left as it was; a slot may be read into several rows.
  */
-int mpic_q4_read(mpic_ctx* ctx, const void* cache, int64_t n_slots, const int32_t* slots, int64_t n_rows,
-                 void* k, int64_t k_stride, void* v, int64_t v_stride, void* stream);
+int mpic_q4_read(mpic_ctx* ctx, const void* cache, int64_t cache_bytes, int64_t n_slots,
+                 const int32_t* slots, int64_t n_rows, void* k, int64_t k_stride, void* v,
+                 int64_t v_stride, void* stream);
 
 /*
  * Attention over contexts held in 4 bits.  Request b has lens[b] tokens, token j of them in slot
@@ -131,8 +134,8 @@ int mpic_q4_read(mpic_ctx* ctx, const void* cache, int64_t n_slots, const int32_
 int mpic_q4_attn_workspace(const mpic_ctx* ctx, int32_t n_requests, int64_t n_rows, int32_t max_q,
                            int64_t max_len, int64_t* bytes);
 int mpic_q4_attn(mpic_ctx* ctx, const void* q, int64_t q_stride, int64_t n_rows, const int32_t* q_off,
-                 int32_t max_q, const void* cache, int64_t n_slots, const int32_t* page_table,
-                 int64_t table_width, int32_t page_size, const int32_t* lens, int32_t n_requests,
+                 int32_t max_q, const void* cache, int64_t cache_bytes, int64_t n_slots,
+                 const int32_t* page_table, int64_t table_width, int32_t page_size, const int32_t* lens, int32_t n_requests,
                  int64_t max_len, double softmax_scale, void* out, float* lse, void* workspace,
                  int64_t workspace_bytes, void* stream);
 

@@ -127,14 +127,14 @@ def load_library():
     lib.mpic_position_rows.restype = C.c_int
     lib.mpic_q4_bytes.argtypes = [vp, i64, C.POINTER(i64)]
     lib.mpic_q4_bytes.restype = C.c_int
-    lib.mpic_q4_write.argtypes = [vp, vp, i64, vp, i64, i64, vp, vp, i64, vp]
+    lib.mpic_q4_write.argtypes = [vp, vp, i64, vp, i64, i64, vp, vp, i64, i64, vp]
     lib.mpic_q4_write.restype = C.c_int
-    lib.mpic_q4_read.argtypes = [vp, vp, i64, vp, i64, vp, i64, vp, i64, vp]
+    lib.mpic_q4_read.argtypes = [vp, vp, i64, i64, vp, i64, vp, i64, vp, i64, vp]
     lib.mpic_q4_read.restype = C.c_int
     lib.mpic_q4_attn_workspace.argtypes = [vp, i32, i64, i32, i64, C.POINTER(i64)]
     lib.mpic_q4_attn_workspace.restype = C.c_int
-    lib.mpic_q4_attn.argtypes = [vp, vp, i64, i64, vp, i32, vp, i64, vp, i64, i32, vp, i32, i64, C.c_double, vp, vp, vp,
-                                 i64, vp]
+    lib.mpic_q4_attn.argtypes = [vp, vp, i64, i64, vp, i32, vp, i64, i64, vp, i64, i32, vp, i32, i64, C.c_double, vp, vp,
+                                 vp, i64, vp]
     lib.mpic_q4_attn.restype = C.c_int
     lib.mpic_strerror.argtypes = [C.c_int]
     lib.mpic_strerror.restype = C.c_char_p
@@ -414,39 +414,45 @@ def mpic_rank_tokens(dist, n_top):
     return out
 
 
-def _rows(ctx_rows, name):
-    """Elements from one row to the next of a [rows][heads][D] tensor whose rows are contiguous."""
-    t = ctx_rows
-    if t.dim() != 3 or t.stride(2) != 1 or t.stride(1) != t.shape[2]:
+def _row_stride(t, shape, name):
+    """Elements from one row to the next of a [rows][heads][D] tensor of that shape whose rows are contiguous."""
+    row, head, one = t.stride()
+    n, heads, d = shape
+    if one != 1 or head != d:
         raise ValueError(f"{name} must be [rows][heads][D] with contiguous rows")
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+    return row if n > 1 else heads * d
 
 
-def _i32_dense(t, name):
-    if t is not None and (t.element_size() != 4 or not t.is_contiguous()):
-        raise ValueError(f"{name} must be a contiguous int32 tensor")
-    return _ptr(t)
+def _int32(t, n, name):
+    """Address of a contiguous int32 tensor of n elements (None: a null pointer)."""
+    if t is None:
+        return None
+    if t.numel() != n or t.element_size() != 4 or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 tensor of {n} elements")
+    return t.data_ptr()
 
 
 def mpic_position_rows(ctx, q, k, pos, q_out, k_out, q_weight=None, k_weight=None, eps=None, pair_axis=None, stream=None):
     """Norms (eps not None) and rotation of fresh rows: q [n][Hq][D] and k [n][Hkv][D] (rows may be strided) to the positions
     pos [n_axes][n] (or [n]); pair_axis names the axis of every pair.  q_out and k_out may be q and k."""
-    n, n_axes = q.shape[0], 1 if pos.dim() == 1 else pos.shape[0]
-    if k.shape[0] != n or q_out.shape != q.shape or k_out.shape != k.shape or pos.shape[-1] != n:
-        raise ValueError("q, k, pos, q_out and k_out must have the same rows")
+    qs, ks = q.shape, k.shape
+    n = qs[0]
+    n_axes = 1 if pos.dim() == 1 else pos.shape[0]
+    if ks[0] != n or q_out.shape != qs or k_out.shape != ks:
+        raise ValueError("q, k, q_out and k_out must have the same rows")
+    axis = None
     if pair_axis is not None:
-        if len(pair_axis) != q.shape[2] // 2:
+        if len(pair_axis) != qs[2] // 2:
             raise ValueError("pair_axis must name an axis for each of the D / 2 pairs")
         keep, axis = _i32_array(pair_axis)
-    else:
-        axis = None
-    if eps is not None and eps < 0:
+    if eps is None:
+        eps = -1.0
+    elif eps < 0:
         raise ValueError("eps must not be negative")
-    rc = load_library().mpic_position_rows(ctx, _ptr(q), _rows(q, "q"), _ptr(k), _rows(k, "k"), n, _i32_dense(pos, "pos"),
-                                           n_axes, axis, _ptr(q_weight), _ptr(k_weight), -1.0 if eps is None else float(eps),
-                                           _ptr(q_out), _rows(q_out, "q_out"), _ptr(k_out), _rows(k_out, "k_out"),
-                                           _stream(stream))
-    _check(rc, ctx)
+    _check(load_library().mpic_position_rows(
+        ctx, q.data_ptr(), _row_stride(q, qs, "q"), k.data_ptr(), _row_stride(k, ks, "k"), n, _int32(pos, n_axes * n, "pos"),
+        n_axes, axis, _ptr(q_weight), _ptr(k_weight), eps, q_out.data_ptr(), _row_stride(q_out, qs, "q_out"), k_out.data_ptr(),
+        _row_stride(k_out, ks, "k_out"), _stream(stream)), ctx)
 
 
 def mpic_q4_bytes(ctx, n_slots):
@@ -456,29 +462,30 @@ def mpic_q4_bytes(ctx, n_slots):
     return n.value
 
 
-def _check_cache(ctx, cache, n_slots):
-    if cache.numel() * cache.element_size() < mpic_q4_bytes(ctx, n_slots) or not cache.is_contiguous():
-        raise ValueError("cache must be contiguous and hold mpic_q4_bytes(n_slots) bytes")
+def _cache_bytes(cache):
+    if not cache.is_contiguous():
+        raise ValueError("cache must be contiguous")
+    return cache.numel() * cache.element_size()
 
 
 def mpic_q4_write(ctx, k, v, slots, cache, n_slots, stream=None):
     """Row r of k and v ([n][Hkv][D], rows may be strided) goes to slot slots[r] (None: slot r) of the cache."""
-    _check_cache(ctx, cache, n_slots)
-    if k.shape != v.shape or (slots is not None and slots.numel() != k.shape[0]):
-        raise ValueError("k, v and slots must have the same rows")
-    rc = load_library().mpic_q4_write(ctx, _ptr(k), _rows(k, "k"), _ptr(v), _rows(v, "v"), k.shape[0],
-                                      _i32_dense(slots, "slots"), _ptr(cache), int(n_slots), _stream(stream))
-    _check(rc, ctx)
+    shape = k.shape
+    if v.shape != shape:
+        raise ValueError("k and v must have the same shape")
+    _check(load_library().mpic_q4_write(
+        ctx, k.data_ptr(), _row_stride(k, shape, "k"), v.data_ptr(), _row_stride(v, shape, "v"), shape[0],
+        _int32(slots, shape[0], "slots"), cache.data_ptr(), _cache_bytes(cache), n_slots, _stream(stream)), ctx)
 
 
 def mpic_q4_read(ctx, cache, n_slots, slots, k, v, stream=None):
     """Rows of k and v = the values that the slots hold; rows without a slot in the cache are left as they were."""
-    _check_cache(ctx, cache, n_slots)
-    if k.shape != v.shape or (slots is not None and slots.numel() != k.shape[0]):
-        raise ValueError("k, v and slots must have the same rows")
-    rc = load_library().mpic_q4_read(ctx, _ptr(cache), int(n_slots), _i32_dense(slots, "slots"), k.shape[0], _ptr(k),
-                                     _rows(k, "k"), _ptr(v), _rows(v, "v"), _stream(stream))
-    _check(rc, ctx)
+    shape = k.shape
+    if v.shape != shape:
+        raise ValueError("k and v must have the same shape")
+    _check(load_library().mpic_q4_read(
+        ctx, cache.data_ptr(), _cache_bytes(cache), n_slots, _int32(slots, shape[0], "slots"), shape[0], k.data_ptr(),
+        _row_stride(k, shape, "k"), v.data_ptr(), _row_stride(v, shape, "v"), _stream(stream)), ctx)
 
 
 def mpic_q4_attn_workspace(ctx, n_requests, n_rows, max_q, max_len):
@@ -493,19 +500,16 @@ def mpic_q4_attn(ctx, q, cache, n_slots, page_table, page_size, lens, softmax_sc
     """Attention over contexts in 4 bits: q [n_rows][Hq][D] (rows may be strided), page_table [B][width], lens [B], with
     several queries per request q_off [B + 1]; all of them int32 device tensors.  workspace: a device tensor of
     mpic_q4_attn_workspace bytes."""
-    _check_cache(ctx, cache, n_slots)
-    b, width = page_table.shape
-    if out.shape != q.shape or not out.is_contiguous() or lens.numel() != b or (q_off is not None and q_off.numel() != b + 1):
-        raise ValueError("out must be contiguous and like q, lens [B], q_off [B + 1]")
-    if lse is not None and (tuple(lse.shape) != tuple(q.shape[:2]) or lse.element_size() != 4 or not lse.is_contiguous()):
+    shape, (b, width) = q.shape, page_table.shape
+    if out.shape != shape or not out.is_contiguous():
+        raise ValueError("out must be contiguous and like q")
+    if lse is not None and (lse.numel() != shape[0] * shape[1] or lse.element_size() != 4 or not lse.is_contiguous()):
         raise ValueError("lse must be a contiguous float32 [n_rows][Hq] tensor")
-    rc = load_library().mpic_q4_attn(ctx, _ptr(q), _rows(q, "q"), q.shape[0], _i32_dense(q_off, "q_off"), int(max_q),
-                                     _ptr(cache), int(n_slots), _i32_dense(page_table, "page_table"), width, int(page_size),
-                                     _i32_dense(lens, "lens"), b, width * int(page_size) if max_len is None else int(max_len),
-                                     float(softmax_scale), _ptr(out), _ptr(lse), _ptr(workspace),
-                                     0 if workspace is None else workspace.numel() * workspace.element_size(),
-                                     _stream(stream))
-    _check(rc, ctx)
+    _check(load_library().mpic_q4_attn(
+        ctx, q.data_ptr(), _row_stride(q, shape, "q"), shape[0], _int32(q_off, b + 1, "q_off"), max_q, cache.data_ptr(),
+        _cache_bytes(cache), n_slots, _int32(page_table, b * width, "page_table"), width, page_size, _int32(lens, b, "lens"), b,
+        width * page_size if max_len is None else max_len, softmax_scale, out.data_ptr(), _ptr(lse), _ptr(workspace),
+        0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)), ctx)
 
 
 MPIC_TIER_MISSING, MPIC_TIER_HBM, MPIC_TIER_HOST, MPIC_TIER_DISK = 0, 1, 2, 3

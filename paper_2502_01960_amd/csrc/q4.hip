@@ -253,7 +253,7 @@ constexpr int kMaxGridY = 65535;
 
 // Checks shared by both directions; fills *a and sets *go if there is anything to do.
 int rows_args(mpic_ctx* ctx, const char* what, const void* k, int64_t k_stride, const void* v, int64_t v_stride, int64_t n_rows,
-              const int32_t* slots, const void* cache, int64_t n_slots, RowsArgs* a, bool* go) {
+              const int32_t* slots, const void* cache, int64_t cache_bytes, int64_t n_slots, RowsArgs* a, bool* go) {
   const mpic_config& c = ctx->cfg;
   const auto invalid = [&](const char* why) { return fail(ctx, MPIC_ERR_INVALID, std::string(what) + ": " + why); };
   const int64_t elem = c.dtype == MPIC_F32 ? 4 : 2, row = static_cast<int64_t>(c.n_kv_heads) * c.head_dim;
@@ -263,6 +263,7 @@ int rows_args(mpic_ctx* ctx, const char* what, const void* k, int64_t k_stride, 
   if (k_stride < row || v_stride < row || k_stride * elem % 16 || v_stride * elem % 16)
     return invalid("strides must hold a row and be multiples of 16 bytes");
   if (!slots && n_rows > n_slots) return invalid("more rows than slots");
+  if (cache_bytes < q4::cache_bytes(c.dtype == MPIC_F32, c.head_dim, c.n_kv_heads, n_slots)) return invalid("the cache is smaller than its slots");
   if (n_rows == 0 || n_slots == 0) return MPIC_OK;  // (no row has a slot)
   if (!k || !v || !cache) return invalid("null buffer");
   if ((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v) | reinterpret_cast<uintptr_t>(cache)) & 15)
@@ -306,22 +307,22 @@ extern "C" int mpic_q4_bytes(const mpic_ctx* ctx, int64_t n_slots, int64_t* byte
   } while (0)
 
 extern "C" int mpic_q4_write(mpic_ctx* ctx, const void* k, int64_t k_stride, const void* v, int64_t v_stride, int64_t n_rows,
-                             const int32_t* slots, void* cache, int64_t n_slots, void* stream) {
+                             const int32_t* slots, void* cache, int64_t cache_bytes, int64_t n_slots, void* stream) {
   if (!ctx) return MPIC_ERR_INVALID;
   mpic::RowsArgs a{};
   bool go;
-  const int rc = mpic::rows_args(ctx, "q4_write", k, k_stride, v, v_stride, n_rows, slots, cache, n_slots, &a, &go);
+  const int rc = mpic::rows_args(ctx, "q4_write", k, k_stride, v, v_stride, n_rows, slots, cache, cache_bytes, n_slots, &a, &go);
   if (rc != MPIC_OK || !go) return rc;
   MPIC_Q4_ROWS(q4_write_kernel, a, static_cast<hipStream_t>(stream));
   return MPIC_OK;
 }
 
-extern "C" int mpic_q4_read(mpic_ctx* ctx, const void* cache, int64_t n_slots, const int32_t* slots, int64_t n_rows, void* k,
-                            int64_t k_stride, void* v, int64_t v_stride, void* stream) {
+extern "C" int mpic_q4_read(mpic_ctx* ctx, const void* cache, int64_t cache_bytes, int64_t n_slots, const int32_t* slots,
+                            int64_t n_rows, void* k, int64_t k_stride, void* v, int64_t v_stride, void* stream) {
   if (!ctx) return MPIC_ERR_INVALID;
   mpic::RowsArgs a{};
   bool go;
-  const int rc = mpic::rows_args(ctx, "q4_read", k, k_stride, v, v_stride, n_rows, slots, cache, n_slots, &a, &go);
+  const int rc = mpic::rows_args(ctx, "q4_read", k, k_stride, v, v_stride, n_rows, slots, cache, cache_bytes, n_slots, &a, &go);
   if (rc != MPIC_OK || !go) return rc;
   MPIC_Q4_ROWS(q4_read_kernel, a, static_cast<hipStream_t>(stream));
   return MPIC_OK;

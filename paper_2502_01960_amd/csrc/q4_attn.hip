@@ -653,8 +653,8 @@ extern "C" int mpic_q4_attn_workspace(const mpic_ctx* ctx, int32_t n_requests, i
 }
 
 extern "C" int mpic_q4_attn(mpic_ctx* ctx, const void* q, int64_t q_stride, int64_t n_rows, const int32_t* q_off, int32_t max_q,
-                            const void* cache, int64_t n_slots, const int32_t* page_table, int64_t table_width,
-                            int32_t page_size, const int32_t* lens, int32_t n_requests, int64_t max_len, double softmax_scale,
+                            const void* cache, int64_t cache_bytes, int64_t n_slots, const int32_t* page_table,
+                            int64_t table_width, int32_t page_size, const int32_t* lens, int32_t n_requests, int64_t max_len, double softmax_scale,
                             void* out, float* lse, void* workspace, int64_t workspace_bytes, void* stream_) {
   using namespace mpic;
   if (!ctx) return MPIC_ERR_INVALID;
@@ -669,6 +669,7 @@ extern "C" int mpic_q4_attn(mpic_ctx* ctx, const void* q, int64_t q_stride, int6
   if (!(softmax_scale > 0.0) || !std::isfinite(softmax_scale)) return invalid("q4_attn: softmax_scale must be finite and positive");
   if (q_stride < static_cast<int64_t>(c.n_q_heads) * c.head_dim || q_stride * elem % 16)
     return invalid("q4_attn: q_stride must hold a row and be a multiple of 16 bytes");
+  if (cache_bytes < q4::cache_bytes(c.dtype == MPIC_F32, c.head_dim, c.n_kv_heads, n_slots)) return invalid("q4_attn: the cache is smaller than its slots");
   if (n_rows == 0 || n_requests == 0) return MPIC_OK;
   if (!q || !cache || !lens || !out || (max_len > 0 && !page_table)) return invalid("q4_attn: null buffer");
   if (max_len > 0 && n_slots == 0) return invalid("q4_attn: a cache without slots");

@@ -55,10 +55,10 @@ def test_position_rows_refuses(ctx):
 
 
 def _write(ctx, read=False, **kw):
-    a = dict(k=A, k_stride=256, v=A, v_stride=256, n=4, slots=A, cache=A, n_slots=64)
+    a = dict(k=A, k_stride=256, v=A, v_stride=256, n=4, slots=A, cache=A, size=1 << 40, n_slots=64)
     a.update(kw)
     if read:
-        return _lib().mpic_q4_read(ctx.handle, a["cache"], a["n_slots"], a["slots"], a["n"], a["k"], a["k_stride"], a["v"], a["v_stride"], None)
+        return _lib().mpic_q4_read(ctx.handle, a["cache"], a["size"], a["n_slots"], a["slots"], a["n"], a["k"], a["k_stride"], a["v"], a["v_stride"], None)
     return _lib().mpic_q4_write(ctx.handle, *a.values(), None)
 
 
@@ -66,11 +66,11 @@ def _write(ctx, read=False, **kw):
 def test_rows_refuse(ctx, read):
     for kw in (dict(n=-1), dict(n=2 ** 31), dict(n_slots=-1), dict(n_slots=2 ** 31), dict(k_stride=255), dict(k_stride=257),
                dict(v_stride=128), dict(slots=None, n=65), dict(k=None), dict(v=None), dict(cache=None), dict(k=A + 8), dict(v=A + 2),
-               dict(cache=A + 4)):
+               dict(cache=A + 4), dict(size=64 * 2 * 144 - 1), dict(size=0)):
         assert _write(ctx, read, **kw) == INVALID, kw
     assert ("q4_read" if read else "q4_write") in mpic.binding.mpic_last_error(ctx.handle)
-    assert _write(ctx, read, n=0, k=None, v=None, cache=None) == 0
-    assert _write(ctx, read, n_slots=0, cache=None) == 0          # no row has a slot
+    assert _write(ctx, read, n=0, k=None, v=None) == 0
+    assert _write(ctx, read, n_slots=0, cache=None, size=0) == 0          # no row has a slot
     many = mpic.Context(40000, 40000, 128, mpic.MPIC_BF16, 1e4)
     assert _write(many, read, k_stride=40000 * 128, v_stride=40000 * 128) == UNSUPPORTED
 
@@ -87,7 +87,7 @@ def test_bytes():
 
 
 def _attn(ctx, **kw):
-    a = dict(q=A, q_stride=1024, n_rows=3, q_off=None, max_q=1, cache=A, n_slots=64, table=A, width=4, page=16, lens=A, n_requests=3,
+    a = dict(q=A, q_stride=1024, n_rows=3, q_off=None, max_q=1, cache=A, size=1 << 40, n_slots=64, table=A, width=4, page=16, lens=A, n_requests=3,
              max_len=64, scale=0.1, out=A, lse=None, ws=None, ws_bytes=0)
     a.update(kw)
     return _lib().mpic_q4_attn(ctx.handle, *a.values(), None)
@@ -96,7 +96,7 @@ def _attn(ctx, **kw):
 def test_attention_refuses(ctx):
     for kw in (dict(n_rows=-1), dict(n_rows=4), dict(max_q=0), dict(max_q=2), dict(n_requests=-1), dict(max_len=-1), dict(max_len=65),
                dict(max_len=2 ** 31), dict(page=0), dict(page=8), dict(page=24), dict(page=-16), dict(width=-1), dict(width=2 ** 40),
-               dict(n_slots=-1), dict(n_slots=2 ** 31), dict(n_slots=0), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")),
+               dict(n_slots=-1), dict(n_slots=2 ** 31), dict(n_slots=0), dict(size=64 * 2 * 144 - 1), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")),
                dict(scale=float("inf")), dict(q_stride=1023), dict(q_stride=1025), dict(q=None), dict(cache=None), dict(table=None),
                dict(lens=None), dict(out=None), dict(q=A + 8), dict(cache=A + 8), dict(out=A + 2), dict(ws=A + 4),
                dict(max_len=1 << 20, width=1 << 16), dict(max_len=1 << 20, width=1 << 16, ws=A, ws_bytes=100),
@@ -124,8 +124,9 @@ def test_binding_refuses_tensors_that_do_not_fit():
     t = lambda *s: torch.zeros(s, dtype=torch.bfloat16)
     i = lambda *s: torch.zeros(s, dtype=torch.int32)
     cache = torch.zeros(mpic.mpic_q4_bytes(ctx.handle, 32), dtype=torch.uint8)
-    for call in (lambda: mpic.mpic_q4_write(ctx.handle, t(3, 2, 128), t(3, 2, 128), i(3), cache, 33),
-                 lambda: mpic.mpic_q4_write(ctx.handle, t(3, 2, 128), t(2, 2, 128), i(3), cache, 32),
+    with pytest.raises(mpic.MpicError):
+        mpic.mpic_q4_write(ctx.handle, t(3, 2, 128), t(3, 2, 128), i(3), cache, 33, 0)
+    for call in (lambda: mpic.mpic_q4_write(ctx.handle, t(3, 2, 128), t(2, 2, 128), i(3), cache, 32),
                  lambda: mpic.mpic_q4_write(ctx.handle, t(3, 2, 128), t(3, 2, 128), i(2), cache, 32),
                  lambda: mpic.mpic_q4_write(ctx.handle, t(3, 128, 2).transpose(1, 2), t(3, 2, 128), i(3), cache, 32),
                  lambda: mpic.mpic_q4_read(ctx.handle, cache, 32, i(3).long(), t(3, 2, 128), t(3, 2, 128)),
@@ -134,6 +135,7 @@ def test_binding_refuses_tensors_that_do_not_fit():
                  lambda: mpic.mpic_position_rows(ctx.handle, t(3, 4, 128), t(3, 2, 128), i(1, 3), t(3, 4, 128), t(3, 2, 128), eps=-1.0),
                  lambda: mpic.mpic_q4_attn(ctx.handle, t(3, 4, 128), cache, 32, i(3, 2), 16, i(2), 0.1, t(3, 4, 128)),
                  lambda: mpic.mpic_q4_attn(ctx.handle, t(3, 4, 128), cache, 32, i(3, 2), 16, i(3), 0.1, t(3, 4, 128), q_off=i(3)),
-                 lambda: mpic.mpic_q4_attn(ctx.handle, t(3, 4, 128), cache, 32, i(3, 2), 16, i(3), 0.1, t(3, 4, 128), lse=t(3, 4))):
+                 lambda: mpic.mpic_q4_attn(ctx.handle, t(3, 4, 128), cache, 32, i(3, 2), 16, i(3), 0.1, t(3, 4, 128), lse=t(3, 4)),
+                 lambda: mpic.mpic_q4_read(ctx.handle, cache[::2], 2, i(3), t(3, 2, 128), t(3, 2, 128))):
         with pytest.raises(ValueError):
             call()
