@@ -24,7 +24,7 @@ struct RowsArgs {
   char* cache;
   const int32_t* slots;
   int64_t n_rows, n_slots, k_stride, v_stride;  // strides in bytes
-  int32_t n_heads;
+  uint32_t n_heads;
 };
 
 // Slot of a row, -1 for rows that are left out
@@ -39,39 +39,154 @@ __device__ inline char* block_of(const RowsArgs& a, int slot, int head) {
   return a.cache + (static_cast<int64_t>(slot >> 4) * a.n_heads + head) * Block<T, D>::kBytes;
 }
 
-// What a group's values share.  `nan`: one of them is no number.
+// Minimum and maximum as single instructions (fminf and fmaxf make a second one of every operand that may be a signalling
+// NaN; what is no number is looked for separately).
+__device__ inline float min3(float a, float b, float c) {
+  float r;
+  asm("v_min3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+__device__ inline float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+struct Range {
+  float low, high;
+  bool nan;  // of this lane's values: one is no number
+};
+template <int N>
+__device__ inline Range range_of(const float (&x)[N]) {
+  Range r = {x[0], x[0], false};
+#pragma unroll
+  for (int e = 0; e < N; e += 2) {
+    r.low = min3(r.low, x[e], x[e + 1]);
+    r.high = max3(r.high, x[e], x[e + 1]);
+    r.nan |= __builtin_isunordered(x[e], x[e + 1]);
+  }
+  return r;
+}
+// over lanes l, l ^ 16, l ^ 32, l ^ 48 (a swap of two copies leaves the one half's values in one, the other's in the other)
+__device__ inline Range range_across_quarters(Range r) {
+  auto both = [](float x, bool rows, float* y) {
+    const unsigned u = __builtin_bit_cast(unsigned, x);
+    const auto p = rows ? __builtin_amdgcn_permlane16_swap(u, u, false, false) : __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    const unsigned p0 = p[0], p1 = p[1];
+    y[0] = __builtin_bit_cast(float, p0);
+    y[1] = __builtin_bit_cast(float, p1);
+  };
+#pragma unroll
+  for (int step = 0; step < 2; ++step) {
+    float l[2], h[2];
+    both(r.low, step == 0, l);
+    both(r.high, step == 0, h);
+    r.low = min3(l[0], l[0], l[1]);
+    r.high = max3(h[0], h[0], h[1]);
+  }
+  return r;
+}
+// over the sixteen lanes of a row, for four ranges: rotations by 8, 4, 2 and 1, interleaved so that no instruction follows
+// within two of the one whose result it fetches from other lanes
+#define MPIC_STEP(n)                                                        \
+  "v_min_f32_dpp %0, %0, %0 row_ror:" #n " row_mask:0xf bank_mask:0xf\n\t" \
+  "v_max_f32_dpp %4, %4, %4 row_ror:" #n " row_mask:0xf bank_mask:0xf\n\t" \
+  "v_min_f32_dpp %1, %1, %1 row_ror:" #n " row_mask:0xf bank_mask:0xf\n\t" \
+  "v_max_f32_dpp %5, %5, %5 row_ror:" #n " row_mask:0xf bank_mask:0xf\n\t" \
+  "v_min_f32_dpp %2, %2, %2 row_ror:" #n " row_mask:0xf bank_mask:0xf\n\t" \
+  "v_max_f32_dpp %6, %6, %6 row_ror:" #n " row_mask:0xf bank_mask:0xf\n\t" \
+  "v_min_f32_dpp %3, %3, %3 row_ror:" #n " row_mask:0xf bank_mask:0xf\n\t" \
+  "v_max_f32_dpp %7, %7, %7 row_ror:" #n " row_mask:0xf bank_mask:0xf\n\t"
+__device__ inline void ranges_across_row(Range (&r)[4]) {
+  asm("s_nop 1\n\t" MPIC_STEP(8) MPIC_STEP(4) MPIC_STEP(2) MPIC_STEP(1) "s_nop 0"
+      : "+v"(r[0].low), "+v"(r[1].low), "+v"(r[2].low), "+v"(r[3].low), "+v"(r[0].high), "+v"(r[1].high), "+v"(r[2].high), "+v"(r[3].high));
+}
+#undef MPIC_STEP
+
+// What a group's values share.  range / 15 by the product with RN(1/15) and one step of the remainder, which rounds it
+// correctly; the reciprocal of the scale is a little too large (see code_of).
 struct Coding {
   float low, scale, inv;
 };
-template <typename T>
-__device__ inline Coding coding_of(float low, float high, bool nan) {
-  const float range = high - low;
-  if (nan || !(range < INFINITY)) return Coding{NAN, NAN, 0.f};  // (infinities and ranges beyond fp32 alike)
-  const float scale = static_cast<float>(static_cast<T>(range / 15.f));
-  if (!(scale >= q4::kLeastScale)) return Coding{low, 0.f, 0.f};
-  return Coding{low, scale, 1.f / scale};
-}
-
-// The whole number nearest to (x - low) / scale, halves upwards.  The product with the reciprocal is off by some 2^-22 at
-// most, so the candidate is off by one at most, and the remainder d - code * scale (exact: both are multiples of the
-// smaller one's last place, and it is no larger than about a scale) tells on which side of a border the value lies.
-__device__ inline uint32_t code_of(float x, const Coding& c) {
-  const float d = x - c.low;
-  float code = floorf(fmaf(d, c.inv, 0.5f));
-  const float e = fmaf(-code, c.scale, d), half = 0.5f * c.scale;
-  code += e >= half ? 1.f : 0.f;
-  code -= e < -half ? 1.f : 0.f;
-  return c.inv == 0.f ? 0u : min(static_cast<uint32_t>(static_cast<int32_t>(code)), 15u);
-}
-
-// n values of T at p as floats (n * sizeof(T) bytes, 8 or 16 byte units)
+// `lanes`: those that share this lane's groups.  Returns whether a group of the wavefront is flat or not finite.
 template <typename T, int N>
-__device__ inline void load_values(const char* p, float (&x)[N]) {
-  typedef T vec __attribute__((ext_vector_type(N), aligned(8)));
-  const vec v = *reinterpret_cast<const vec*>(p);
+__device__ inline bool codings_of(const Range (&r)[N], uint64_t lanes, Coding (&c)[N]) {
+  bool odd = false;
+  constexpr float kFifteenth = 1.f / 15.f;
 #pragma unroll
-  for (int e = 0; e < N; ++e) x[e] = static_cast<float>(v[e]);
+  for (int i = 0; i < N; ++i) {
+    const float range = r[i].high - r[i].low;
+    float q = range * kFifteenth;
+    q = fmaf(fmaf(-15.f, q, range), kFifteenth, q);
+    c[i].low = r[i].low;
+    c[i].scale = static_cast<float>(static_cast<T>(q));
+    c[i].inv = __builtin_amdgcn_rcpf(c[i].scale) * (1.f + 0x1p-20f);
+    odd |= r[i].nan || !(range < INFINITY) || !(c[i].scale >= q4::kLeastScale);
+  }
+  if (!__any(odd)) return false;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    if ((__ballot(r[i].nan) & lanes) || !(r[i].high - r[i].low < INFINITY))  // (infinities and ranges beyond fp32 alike)
+      c[i] = Coding{NAN, NAN, 0.f};
+    else if (!(c[i].scale >= q4::kLeastScale))
+      c[i] = Coding{r[i].low, 0.f, 0.f};
+  }
+  return true;
 }
+
+// The whole number nearest to (x - low) / scale, halves upwards.  The candidate is the product with the reciprocal, rounded by
+// an addition that leaves it in the last bits of a float.  The reciprocal is 2^-20 too large, more than it can be off: so
+// quotients halfway between two codes, which are common where values have few bits, go up as they should, and the
+// only candidates that are wrong are one too large, for quotients within 2^-16 below a border.  The remainder
+// e = d - code * scale is exact (both are multiples of the smaller one's last place, and it is no larger than about a scale)
+// and tells those; `check` collects them, and a wavefront that has any (or a group that is flat or not finite) goes through
+// exact_code.  The greatest value gets 15: rounding the scale makes its quotient 15.06 at most.
+constexpr float kWhole = 8388608.f;  // 2^23
+struct Codes {
+  uint32_t word;
+  bool check;
+  // Codes go in from the last nibble of a word to the first.  What the float's other bits add to the word is the same for
+  // every code and comes off at the end.
+  __device__ inline void push(float x, const Coding& c) {
+    const float d = x - c.low;
+    const float t = fmaf(d, c.inv, kWhole);
+    const float e = fmaf(kWhole - t, c.scale, d);
+    check |= e < -0.5f * c.scale;
+    word = (word << 4) + __builtin_bit_cast(uint32_t, t);
+  }
+  static constexpr uint32_t kRest = 0x4B000000u + 0xB0000000u;  // sum of 0x4B000000 << 4 n, n = 0 .. 7, modulo 2^32
+  __device__ inline uint32_t done() const { return word - kRest; }
+};
+__device__ inline uint32_t exact_code(float x, const Coding& c) {
+  const float d = x - c.low;
+  const float code = fmaf(d, c.inv, kWhole) - kWhole;
+  const uint32_t n = static_cast<uint32_t>(static_cast<int>(code) - (fmaf(-code, c.scale, d) < -0.5f * c.scale ? 1 : 0));
+  return c.inv == 0.f ? 0u : n;
+}
+
+// N values of T, kept as they are in memory: bf16 values take half the registers of floats, and are widened where they are
+// needed, once for the range and once for the codes (more wavefronts fit a SIMD)
+template <typename T, int N>
+struct Values {
+  typedef T vec __attribute__((ext_vector_type(N), aligned(8)));
+  typedef uint32_t bits __attribute__((ext_vector_type(N * sizeof(T) / 4)));
+  bits raw;
+  __device__ inline void load(const char* p) { raw = __builtin_bit_cast(bits, *reinterpret_cast<const vec*>(p)); }
+  __device__ inline void widen(float (&x)[N]) const {
+    const vec v = __builtin_bit_cast(vec, raw);
+#pragma unroll
+    for (int e = 0; e < N; ++e) x[e] = static_cast<float>(v[e]);
+  }
+  // what was widened before is not kept
+  __device__ inline void forget() {
+    if (sizeof(T) == 2)
+#pragma unroll
+      for (int i = 0; i < static_cast<int>(N * sizeof(T) / 4); ++i) {
+        uint32_t u = raw[i];
+        asm volatile("" : "+v"(u));
+        raw[i] = u;
+      }
+  }
+};
 template <typename T, int N>
 __device__ inline void store_values(char* p, const float (&x)[N]) {
   typedef T vec __attribute__((ext_vector_type(N), aligned(8)));
@@ -90,39 +205,52 @@ __device__ inline void write_keys(const RowsArgs& a, int64_t row0, int head, int
   using B = Block<T, D>;
   const int t = lane & 15, c = lane >> 4;
   const int slot = slot_of(a, row0 + t);
-  // rows that are left out take part in the exchanges (with zeros) and store nothing
+  // rows that are left out take part in the exchanges (with a row that is there) and store nothing
+  const char* row = a.k + min(row0 + t, a.n_rows - 1) * a.k_stride + (head * D + 16 * c) * sizeof(T);
   char* block = block_of<T, D>(a, max(slot, 0), head);
+  Values<T, 16> v[B::kGroups];
+#pragma unroll
+  for (int g = 0; g < B::kGroups; ++g) v[g].load(row + g * kGroup * sizeof(T));
+  Range range[B::kGroups];
+  float x[16];
+#pragma unroll
+  for (int g = 0; g < B::kGroups; ++g) {
+    v[g].widen(x);
+    range[g] = range_across_quarters(range_of(x));
+    v[g].forget();
+  }
+  Coding code[B::kGroups];
+  bool check = codings_of<T>(range, 0x0001000100010001ull << t, code);
   uint32_t words[B::kGroups * 2];
 #pragma unroll
   for (int g = 0; g < B::kGroups; ++g) {
-    float x[16] = {};
-    if (slot >= 0) load_values<T, 16>(a.k + (row0 + t) * a.k_stride + (head * D + g * kGroup + 16 * c) * sizeof(T), x);
-    float low = x[0], high = x[0];
-    bool nan = false;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      low = fminf(low, x[e]);
-      high = fmaxf(high, x[e]);
-      nan |= x[e] != x[e];
-    }
-#pragma unroll
-    for (int off = 16; off < 64; off <<= 1) {
-      low = fminf(low, __shfl_xor(low, off));
-      high = fmaxf(high, __shfl_xor(high, off));
-    }
-    nan = (__ballot(nan) >> t & 0x0001000100010001ull) != 0;
-    const Coding code = coding_of<T>(low, high, nan);
+    v[g].widen(x);
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
-      uint32_t word = 0;
+      Codes codes = {0, check};
 #pragma unroll
-      for (int n = 0; n < 4; ++n)
-        word |= code_of(x[8 * w + 2 * n], code) << (4 * n) | code_of(x[8 * w + 2 * n + 1], code) << (16 + 4 * n);
-      words[2 * g + w] = word;
+      for (int n = 7; n >= 0; --n) codes.push(x[8 * w + (n < 4 ? 2 * n : 2 * n - 7)], code[g]);
+      words[2 * g + w] = codes.done();
+      check = codes.check;
     }
-    if (slot >= 0 && c == 0)
-      reinterpret_cast<Pair<T>*>(block + B::kKPairs)[g * kTokens + (slot & 15)] = Pair<T>{static_cast<T>(code.scale), static_cast<T>(code.low)};
   }
+  if (__any(check))
+#pragma unroll
+    for (int g = 0; g < B::kGroups; ++g) {
+      v[g].forget();
+      v[g].widen(x);
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        words[2 * g + w] = 0;
+#pragma unroll
+        for (int n = 7; n >= 0; --n)
+          words[2 * g + w] = words[2 * g + w] << 4 | exact_code(x[8 * w + (n < 4 ? 2 * n : 2 * n - 7)], code[g]);
+      }
+    }
+  if (slot >= 0 && c == 0)
+#pragma unroll
+    for (int g = 0; g < B::kGroups; ++g)
+      reinterpret_cast<Pair<T>*>(block + B::kKPairs)[g * kTokens + (slot & 15)] = Pair<T>{static_cast<T>(code[g].scale), static_cast<T>(code[g].low)};
   if (slot < 0) return;
   uint32_t* dst = reinterpret_cast<uint32_t*>(block + (c * kTokens + (slot & 15)) * B::kLaneBytes);
 #pragma unroll
@@ -134,31 +262,61 @@ __device__ inline void write_values(const RowsArgs& a, int64_t row0, int head, i
   using B = Block<T, D>;
   const int i = lane & 15, quad = lane >> 4;
   int slot[4];
-  uint32_t words[B::kGroups * 2] = {};
+  Values<T, 4> v[B::kGroups][4];
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
     const int64_t row = row0 + 4 * quad + r;
     slot[r] = slot_of(a, row);
 #pragma unroll
-    for (int g = 0; g < B::kGroups; ++g) {
-      float x[4] = {};
-      if (slot[r] >= 0) load_values<T, 4>(a.v + row * a.v_stride + (head * D + g * kGroup + 4 * i) * sizeof(T), x);
-      float low = fminf(fminf(x[0], x[1]), fminf(x[2], x[3])), high = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
-      bool nan = x[0] != x[0] || x[1] != x[1] || x[2] != x[2] || x[3] != x[3];
+    for (int g = 0; g < B::kGroups; ++g)
+      v[g][r].load(a.v + min(row, a.n_rows - 1) * a.v_stride + (head * D + g * kGroup + 4 * i) * sizeof(T));
+  }
+  uint32_t words[B::kGroups * 2];
+  Coding code[B::kGroups][4];
+  bool check = false;
+  float x[4][4];
 #pragma unroll
-      for (int off = 1; off < 16; off <<= 1) {
-        low = fminf(low, __shfl_xor(low, off));
-        high = fmaxf(high, __shfl_xor(high, off));
-      }
-      nan = (__ballot(nan) >> (16 * quad) & 0xffffull) != 0;
-      const Coding code = coding_of<T>(low, high, nan);
+  for (int g = 0; g < B::kGroups; ++g) {
+    Range range[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) words[2 * g + e / 2] |= code_of(x[e], code) << (8 * r + 4 * (e & 1));
-      if (slot[r] >= 0 && i == 0)
-        reinterpret_cast<Pair<T>*>(block_of<T, D>(a, slot[r], head) + B::kVPairs)[g * kTokens + (slot[r] & 15)] =
-            Pair<T>{static_cast<T>(code.scale), static_cast<T>(code.low)};
+    for (int r = 0; r < 4; ++r) {
+      v[g][r].widen(x[r]);
+      range[r] = range_of(x[r]);
+    }
+    ranges_across_row(range);
+    check |= codings_of<T>(range, 0xffffull << (16 * quad), code[g]);
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      Codes codes = {0, check};
+#pragma unroll
+      for (int n = 7; n >= 0; --n) codes.push(x[n / 2][2 * w + n % 2], code[g][n / 2]);
+      words[2 * g + w] = codes.done();
+      check = codes.check;
     }
   }
+  if (__any(check))
+#pragma unroll
+    for (int g = 0; g < B::kGroups; ++g) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        v[g][r].forget();
+        v[g][r].widen(x[r]);
+      }
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        words[2 * g + w] = 0;
+#pragma unroll
+        for (int n = 7; n >= 0; --n) words[2 * g + w] = words[2 * g + w] << 4 | exact_code(x[n / 2][2 * w + n % 2], code[g][n / 2]);
+      }
+    }
+  if (i == 0)
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (slot[r] >= 0)
+#pragma unroll
+        for (int g = 0; g < B::kGroups; ++g)
+          reinterpret_cast<Pair<T>*>(block_of<T, D>(a, slot[r], head) + B::kVPairs)[g * kTokens + (slot[r] & 15)] =
+              Pair<T>{static_cast<T>(code[g][r].scale), static_cast<T>(code[g][r].low)};
   // four rows that fill a quad of slots go out as words, any others byte by byte
   const bool whole = slot[0] >= 0 && (slot[0] & 3) == 0 && slot[1] == slot[0] + 1 && slot[2] == slot[0] + 2 && slot[3] == slot[0] + 3;
   if (whole) {
@@ -176,16 +334,18 @@ __device__ inline void write_values(const RowsArgs& a, int64_t row0, int head, i
   }
 }
 
-// A wavefront's 16 rows, and their keys or values of a head: grid (four tiles of rows, head and part)
+// A wavefront's 16 rows, and their keys or values of a head.  Heads come first, so that whole rows are read and written by
+// neighbouring wavefronts.
 struct Item {
   int64_t row0;
   int head;
   bool values;
 };
 __device__ inline bool item_of(const RowsArgs& a, Item* item) {
-  item->row0 = (static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6)) * kTokens;
-  item->head = blockIdx.y >> 1;
-  item->values = blockIdx.y & 1;
+  const uint32_t n = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), th = n / a.n_heads;
+  item->head = static_cast<int>(n % a.n_heads);
+  item->values = th & 1;
+  item->row0 = static_cast<int64_t>(th >> 1) * kTokens;
   return item->row0 < a.n_rows;
 }
 
@@ -249,8 +409,6 @@ __global__ __launch_bounds__(256) void q4_read_kernel(RowsArgs a) {
   }
 }
 
-constexpr int kMaxGridY = 65535;
-
 // Checks shared by both directions; fills *a and sets *go if there is anything to do.
 int rows_args(mpic_ctx* ctx, const char* what, const void* k, int64_t k_stride, const void* v, int64_t v_stride, int64_t n_rows,
               const int32_t* slots, const void* cache, int64_t cache_bytes, int64_t n_slots, RowsArgs* a, bool* go) {
@@ -268,7 +426,8 @@ int rows_args(mpic_ctx* ctx, const char* what, const void* k, int64_t k_stride, 
   if (!k || !v || !cache) return invalid("null buffer");
   if ((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v) | reinterpret_cast<uintptr_t>(cache)) & 15)
     return invalid("buffers must be 16-byte aligned");
-  if (2 * static_cast<int64_t>(c.n_kv_heads) > kMaxGridY) return fail(ctx, MPIC_ERR_UNSUPPORTED, std::string(what) + ": too many heads");
+  if ((n_rows + kTokens - 1) / kTokens * c.n_kv_heads * 2 > INT32_MAX / 64)  // (wavefronts; threads of a launch)
+    return fail(ctx, MPIC_ERR_UNSUPPORTED, std::string(what) + ": too many rows and heads for one launch");
   const int rc = bind_device(ctx);
   if (rc != MPIC_OK) return rc;
   a->k = static_cast<const char*>(k);
@@ -296,7 +455,7 @@ extern "C" int mpic_q4_bytes(const mpic_ctx* ctx, int64_t n_slots, int64_t* byte
 
 #define MPIC_Q4_ROWS(kernel, args, stream)                                                                          \
   do {                                                                                                              \
-    const dim3 grid(static_cast<unsigned>((args.n_rows + 63) / 64), 2 * args.n_heads);                              \
+    const dim3 grid(static_cast<unsigned>(((args.n_rows + mpic::kTokens - 1) / mpic::kTokens * args.n_heads * 2 + 3) / 4)); \
     if (ctx->cfg.dtype == MPIC_BF16)                                                                                \
       hipLaunchKernelGGL((mpic::kernel<__bf16, 128>), grid, dim3(256), 0, stream, args);                            \
     else if (ctx->cfg.head_dim == 128)                                                                              \

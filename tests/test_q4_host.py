@@ -71,8 +71,7 @@ def test_rows_refuse(ctx, read):
     assert ("q4_read" if read else "q4_write") in mpic.binding.mpic_last_error(ctx.handle)
     assert _write(ctx, read, n=0, k=None, v=None) == 0
     assert _write(ctx, read, n_slots=0, cache=None, size=0) == 0          # no row has a slot
-    many = mpic.Context(40000, 40000, 128, mpic.MPIC_BF16, 1e4)
-    assert _write(many, read, k_stride=40000 * 128, v_stride=40000 * 128) == UNSUPPORTED
+    assert _write(ctx, read, n=2 ** 31 - 2, n_slots=2 ** 31 - 2) == UNSUPPORTED
 
 
 def test_bytes():
