@@ -27,6 +27,11 @@ struct RowsArgs {
   uint32_t n_heads;
 };
 
+template <typename T>
+struct Pair {
+  T scale, low;
+};
+
 // Slot of a row, -1 for rows that are left out
 __device__ inline int slot_of(const RowsArgs& a, int64_t row) {
   if (row >= a.n_rows) return -1;
@@ -53,16 +58,16 @@ __device__ inline float max3(float a, float b, float c) {
 }
 struct Range {
   float low, high;
-  bool nan;  // of this lane's values: one is no number
 };
+// *nan: one of the values is no number
 template <int N>
-__device__ inline Range range_of(const float (&x)[N]) {
-  Range r = {x[0], x[0], false};
+__device__ inline Range range_of(const float (&x)[N], bool* nan) {
+  Range r = {x[0], x[0]};
 #pragma unroll
   for (int e = 0; e < N; e += 2) {
     r.low = min3(r.low, x[e], x[e + 1]);
     r.high = max3(r.high, x[e], x[e + 1]);
-    r.nan |= __builtin_isunordered(x[e], x[e + 1]);
+    *nan |= __builtin_isunordered(x[e], x[e + 1]);
   }
   return r;
 }
@@ -107,10 +112,9 @@ __device__ inline void ranges_across_row(Range (&r)[4]) {
 struct Coding {
   float low, scale, inv;
 };
-// `lanes`: those that share this lane's groups.  Returns whether a group of the wavefront is flat or not finite.
+// Sets *odd if a group is flat or its range is not finite (0 / 0 and inf - inf come out as no number).
 template <typename T, int N>
-__device__ inline bool codings_of(const Range (&r)[N], uint64_t lanes, Coding (&c)[N]) {
-  bool odd = false;
+__device__ inline void codings_of(const Range (&r)[N], Coding (&c)[N], bool* odd) {
   constexpr float kFifteenth = 1.f / 15.f;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
@@ -120,17 +124,15 @@ __device__ inline bool codings_of(const Range (&r)[N], uint64_t lanes, Coding (&
     c[i].low = r[i].low;
     c[i].scale = static_cast<float>(static_cast<T>(q));
     c[i].inv = __builtin_amdgcn_rcpf(c[i].scale) * (1.f + 0x1p-20f);
-    odd |= r[i].nan || !(range < INFINITY) || !(c[i].scale >= q4::kLeastScale);
+    *odd |= !(c[i].scale >= q4::kLeastScale);
   }
-  if (!__any(odd)) return false;
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    if ((__ballot(r[i].nan) & lanes) || !(r[i].high - r[i].low < INFINITY))  // (infinities and ranges beyond fp32 alike)
-      c[i] = Coding{NAN, NAN, 0.f};
-    else if (!(c[i].scale >= q4::kLeastScale))
-      c[i] = Coding{r[i].low, 0.f, 0.f};
-  }
-  return true;
+}
+// What such groups get, and groups with a value that is no number: `nan` of any of the `lanes` that share the group
+__device__ inline void settle(Coding* c, bool nan, uint64_t lanes) {
+  if ((__ballot(nan) & lanes) || c->scale != c->scale)
+    *c = Coding{NAN, NAN, 0.f};
+  else if (!(c->scale >= q4::kLeastScale))
+    *c = Coding{c->low, 0.f, 0.f};
 }
 
 // The whole number nearest to (x - low) / scale, halves upwards.  The candidate is the product with the reciprocal, rounded by
@@ -138,30 +140,31 @@ __device__ inline bool codings_of(const Range (&r)[N], uint64_t lanes, Coding (&
 // quotients halfway between two codes, which are common where values have few bits, go up as they should, and the
 // only candidates that are wrong are one too large, for quotients within 2^-16 below a border.  The remainder
 // e = d - code * scale is exact (both are multiples of the smaller one's last place, and it is no larger than about a scale)
-// and tells those; `check` collects them, and a wavefront that has any (or a group that is flat or not finite) goes through
-// exact_code.  The greatest value gets 15: rounding the scale makes its quotient 15.06 at most.
+// and tells those; `check` collects them, and a wavefront that has any (or a group that is flat or not finite) is done
+// once more with care.  The greatest value gets 15: rounding the scale makes its quotient 15.06 at most.
 constexpr float kWhole = 8388608.f;  // 2^23
 struct Codes {
   uint32_t word;
   bool check;
   // Codes go in from the last nibble of a word to the first.  What the float's other bits add to the word is the same for
   // every code and comes off at the end.
+  template <bool kSure>
   __device__ inline void push(float x, const Coding& c) {
     const float d = x - c.low;
     const float t = fmaf(d, c.inv, kWhole);
     const float e = fmaf(kWhole - t, c.scale, d);
-    check |= e < -0.5f * c.scale;
-    word = (word << 4) + __builtin_bit_cast(uint32_t, t);
+    const bool over = e < -0.5f * c.scale;
+    if (!kSure) {
+      check |= over;
+      word = (word << 4) + __builtin_bit_cast(uint32_t, t);
+    } else {
+      word = word << 4 | (c.inv == 0.f ? 0u : static_cast<uint32_t>(static_cast<int>(t - kWhole) - (over ? 1 : 0)));
+    }
   }
-  static constexpr uint32_t kRest = 0x4B000000u + 0xB0000000u;  // sum of 0x4B000000 << 4 n, n = 0 .. 7, modulo 2^32
-  __device__ inline uint32_t done() const { return word - kRest; }
+  static constexpr uint32_t kRest = 0xFB000000u;  // sum of 0x4B000000 << 4 n, n = 0 .. 7, modulo 2^32
+  template <bool kSure>
+  __device__ inline uint32_t done() const { return kSure ? word : word - kRest; }
 };
-__device__ inline uint32_t exact_code(float x, const Coding& c) {
-  const float d = x - c.low;
-  const float code = fmaf(d, c.inv, kWhole) - kWhole;
-  const uint32_t n = static_cast<uint32_t>(static_cast<int>(code) - (fmaf(-code, c.scale, d) < -0.5f * c.scale ? 1 : 0));
-  return c.inv == 0.f ? 0u : n;
-}
 
 // N values of T, kept as they are in memory: bf16 values take half the registers of floats, and are widened where they are
 // needed, once for the range and once for the codes (more wavefronts fit a SIMD)
@@ -195,10 +198,43 @@ __device__ inline void store_values(char* p, const float (&x)[N]) {
   for (int e = 0; e < N; ++e) v[e] = static_cast<T>(x[e]);
   *reinterpret_cast<vec*>(p) = v;
 }
-template <typename T>
-struct Pair {
-  T scale, low;
-};
+
+// Codes and codings of a lane's keys: `row` its values of the first group.  kSure: without a doubt, values read again; returns
+// whether that has to be done in this wavefront.
+template <typename T, int D, bool kSure>
+__device__ inline bool encode_keys(const char* row, int t, Pair<T> (&pairs)[Block<T, D>::kGroups], uint32_t (&words)[Block<T, D>::kGroups * 2]) {
+  constexpr int kGroups = Block<T, D>::kGroups;
+  Values<T, 16> v[kGroups];
+#pragma unroll
+  for (int g = 0; g < kGroups; ++g) v[g].load(row + g * kGroup * sizeof(T));
+  Range range[kGroups];
+  float x[16];
+  bool check = false, nan[kGroups] = {};
+#pragma unroll
+  for (int g = 0; g < kGroups; ++g) {
+    v[g].widen(x);
+    range[g] = range_across_quarters(range_of(x, kSure ? &nan[g] : &check));
+    v[g].forget();
+  }
+  Coding code[kGroups];
+  codings_of<T>(range, code, &check);
+#pragma unroll
+  for (int g = 0; g < kGroups; ++g) {
+    __builtin_amdgcn_sched_barrier(0);  // (a group after the other: fewer registers, more wavefronts)
+    if (kSure) settle(&code[g], nan[g], 0x0001000100010001ull << t);
+    pairs[g] = Pair<T>{static_cast<T>(code[g].scale), static_cast<T>(code[g].low)};
+    v[g].widen(x);
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      Codes codes = {0, check};
+#pragma unroll
+      for (int n = 7; n >= 0; --n) codes.push<kSure>(x[8 * w + (n < 4 ? 2 * n : 2 * n - 7)], code[g]);
+      words[2 * g + w] = codes.done<kSure>();
+      check = codes.check;
+    }
+  }
+  return __any(check);
+}
 
 template <typename T, int D>
 __device__ inline void write_keys(const RowsArgs& a, int64_t row0, int head, int lane) {
@@ -207,116 +243,84 @@ __device__ inline void write_keys(const RowsArgs& a, int64_t row0, int head, int
   const int slot = slot_of(a, row0 + t);
   // rows that are left out take part in the exchanges (with a row that is there) and store nothing
   const char* row = a.k + min(row0 + t, a.n_rows - 1) * a.k_stride + (head * D + 16 * c) * sizeof(T);
-  char* block = block_of<T, D>(a, max(slot, 0), head);
-  Values<T, 16> v[B::kGroups];
-#pragma unroll
-  for (int g = 0; g < B::kGroups; ++g) v[g].load(row + g * kGroup * sizeof(T));
-  Range range[B::kGroups];
-  float x[16];
-#pragma unroll
-  for (int g = 0; g < B::kGroups; ++g) {
-    v[g].widen(x);
-    range[g] = range_across_quarters(range_of(x));
-    v[g].forget();
-  }
-  Coding code[B::kGroups];
-  bool check = codings_of<T>(range, 0x0001000100010001ull << t, code);
+  Pair<T> pairs[B::kGroups];
   uint32_t words[B::kGroups * 2];
-#pragma unroll
-  for (int g = 0; g < B::kGroups; ++g) {
-    v[g].widen(x);
-#pragma unroll
-    for (int w = 0; w < 2; ++w) {
-      Codes codes = {0, check};
-#pragma unroll
-      for (int n = 7; n >= 0; --n) codes.push(x[8 * w + (n < 4 ? 2 * n : 2 * n - 7)], code[g]);
-      words[2 * g + w] = codes.done();
-      check = codes.check;
-    }
-  }
-  if (__any(check))
-#pragma unroll
-    for (int g = 0; g < B::kGroups; ++g) {
-      v[g].forget();
-      v[g].widen(x);
-#pragma unroll
-      for (int w = 0; w < 2; ++w) {
-        words[2 * g + w] = 0;
-#pragma unroll
-        for (int n = 7; n >= 0; --n)
-          words[2 * g + w] = words[2 * g + w] << 4 | exact_code(x[8 * w + (n < 4 ? 2 * n : 2 * n - 7)], code[g]);
-      }
-    }
+  if (encode_keys<T, D, false>(row, t, pairs, words)) encode_keys<T, D, true>(row, t, pairs, words);
+  char* block = block_of<T, D>(a, max(slot, 0), head);
   if (slot >= 0 && c == 0)
 #pragma unroll
     for (int g = 0; g < B::kGroups; ++g)
-      reinterpret_cast<Pair<T>*>(block + B::kKPairs)[g * kTokens + (slot & 15)] = Pair<T>{static_cast<T>(code[g].scale), static_cast<T>(code[g].low)};
+      reinterpret_cast<Pair<T>*>(block + B::kKPairs)[g * kTokens + (slot & 15)] = pairs[g];
   if (slot < 0) return;
   uint32_t* dst = reinterpret_cast<uint32_t*>(block + (c * kTokens + (slot & 15)) * B::kLaneBytes);
 #pragma unroll
   for (int w = 0; w < B::kGroups * 2; ++w) dst[w] = words[w];
 }
 
-template <typename T, int D>
-__device__ inline void write_values(const RowsArgs& a, int64_t row0, int head, int lane) {
-  using B = Block<T, D>;
-  const int i = lane & 15, quad = lane >> 4;
-  int slot[4];
-  Values<T, 4> v[B::kGroups][4];
+// The same of the values of four rows
+template <typename T, int D, bool kSure>
+__device__ inline bool encode_values(const char* const (&row)[4], int quad, Pair<T> (&pairs)[Block<T, D>::kGroups][4],
+                                     uint32_t (&words)[Block<T, D>::kGroups * 2]) {
+  constexpr int kGroups = Block<T, D>::kGroups;
+  Values<T, 4> v[kGroups][4];
 #pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    const int64_t row = row0 + 4 * quad + r;
-    slot[r] = slot_of(a, row);
+  for (int r = 0; r < 4; ++r)
 #pragma unroll
-    for (int g = 0; g < B::kGroups; ++g)
-      v[g][r].load(a.v + min(row, a.n_rows - 1) * a.v_stride + (head * D + g * kGroup + 4 * i) * sizeof(T));
-  }
-  uint32_t words[B::kGroups * 2];
-  Coding code[B::kGroups][4];
+    for (int g = 0; g < kGroups; ++g) v[g][r].load(row[r] + g * kGroup * sizeof(T));
   bool check = false;
-  float x[4][4];
 #pragma unroll
-  for (int g = 0; g < B::kGroups; ++g) {
+  for (int g = 0; g < kGroups; ++g) {
+    __builtin_amdgcn_sched_barrier(0);
+    float x[4][4];
     Range range[4];
+    bool nan[4] = {};
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       v[g][r].widen(x[r]);
-      range[r] = range_of(x[r]);
+      range[r] = range_of(x[r], kSure ? &nan[r] : &check);
     }
     ranges_across_row(range);
-    check |= codings_of<T>(range, 0xffffull << (16 * quad), code[g]);
+    Coding code[4];
+    codings_of<T>(range, code, &check);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      if (kSure) settle(&code[r], nan[r], 0xffffull << (16 * quad));
+      pairs[g][r] = Pair<T>{static_cast<T>(code[r].scale), static_cast<T>(code[r].low)};
+    }
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
       Codes codes = {0, check};
 #pragma unroll
-      for (int n = 7; n >= 0; --n) codes.push(x[n / 2][2 * w + n % 2], code[g][n / 2]);
-      words[2 * g + w] = codes.done();
+      for (int n = 7; n >= 0; --n) codes.push<kSure>(x[n / 2][2 * w + n % 2], code[n / 2]);
+      words[2 * g + w] = codes.done<kSure>();
       check = codes.check;
     }
   }
-  if (__any(check))
+  return __any(check);
+}
+
+template <typename T, int D>
+__device__ inline void write_values(const RowsArgs& a, int64_t row0, int head, int lane) {
+  using B = Block<T, D>;
+  const int i = lane & 15, quad = lane >> 4;
+  const char* row[4];
+  int slot[4];
 #pragma unroll
-    for (int g = 0; g < B::kGroups; ++g) {
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        v[g][r].forget();
-        v[g][r].widen(x[r]);
-      }
-#pragma unroll
-      for (int w = 0; w < 2; ++w) {
-        words[2 * g + w] = 0;
-#pragma unroll
-        for (int n = 7; n >= 0; --n) words[2 * g + w] = words[2 * g + w] << 4 | exact_code(x[n / 2][2 * w + n % 2], code[g][n / 2]);
-      }
-    }
+  for (int r = 0; r < 4; ++r) {
+    const int64_t n = row0 + 4 * quad + r;
+    slot[r] = slot_of(a, n);
+    row[r] = a.v + min(n, a.n_rows - 1) * a.v_stride + (head * D + 4 * i) * sizeof(T);
+  }
+  Pair<T> pairs[B::kGroups][4];
+  uint32_t words[B::kGroups * 2];
+  if (encode_values<T, D, false>(row, quad, pairs, words)) encode_values<T, D, true>(row, quad, pairs, words);
   if (i == 0)
 #pragma unroll
     for (int r = 0; r < 4; ++r)
       if (slot[r] >= 0)
 #pragma unroll
         for (int g = 0; g < B::kGroups; ++g)
-          reinterpret_cast<Pair<T>*>(block_of<T, D>(a, slot[r], head) + B::kVPairs)[g * kTokens + (slot[r] & 15)] =
-              Pair<T>{static_cast<T>(code[g][r].scale), static_cast<T>(code[g][r].low)};
+          reinterpret_cast<Pair<T>*>(block_of<T, D>(a, slot[r], head) + B::kVPairs)[g * kTokens + (slot[r] & 15)] = pairs[g][r];
   // four rows that fill a quad of slots go out as words, any others byte by byte
   const bool whole = slot[0] >= 0 && (slot[0] & 3) == 0 && slot[1] == slot[0] + 1 && slot[2] == slot[0] + 2 && slot[3] == slot[0] + 3;
   if (whole) {
