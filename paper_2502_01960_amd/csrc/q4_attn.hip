@@ -24,85 +24,14 @@
 #include <cmath>
 #include <type_traits>
 
-#include "common.h"
-#include "mpic_q4.h"
-#include "q4.h"
-#include "wave_ops.h"
+#include "q4_attn.h"
 
 namespace mpic {
 namespace {
 
-using q4::Block;
-using q4::kTokens;
+using namespace q4;
 
 constexpr int kWaves = 4;
-constexpr int kUnit = 32;       // tokens a wavefront takes at a time: two blocks
-constexpr float kSlack = 8.0f;  // a column's reference point may lag behind its greatest score by this much, log2 units
-
-struct Q4AttnArgs {
-  const char* q;
-  const char* cache;
-  const int32_t* q_off;
-  const int32_t* table;
-  const int32_t* lens;
-  char* out;
-  float* lse;
-  float* ws_o;    // [rows][Hq][n_splits][D] normalised partial outputs
-  float* ws_lse;  // [rows][Hq][n_splits] their log-sum-exp in log2 units, -inf: nothing seen
-  int64_t n_rows, q_stride, table_width;  // q_stride in bytes
-  int32_t n_blocks, page_blocks, max_q, max_len, n_splits, split_units, n_q_heads, n_kv_heads, group;
-  float scale_log2;  // softmax_scale * log2(e)
-};
-
-// Queries of a request, within what the arguments allow whatever the device arrays hold
-struct Request {
-  int64_t first;  // first row
-  int n, len;
-};
-__device__ inline Request request_of(const Q4AttnArgs& a, int b) {
-  Request r;
-  r.len = min(max(a.lens[b], 0), a.max_len);
-  if (!a.q_off) {
-    r.first = b;
-    r.n = 1;
-  } else {
-    const int64_t lo = min(max(static_cast<int64_t>(a.q_off[b]), int64_t{0}), a.n_rows);
-    const int64_t hi = min(max(static_cast<int64_t>(a.q_off[b + 1]), lo), a.n_rows);
-    r.first = lo;
-    r.n = static_cast<int>(min(hi - lo, static_cast<int64_t>(a.max_q)));
-    // (the queries belong to the last tokens: those beyond max_q are the last of them)
-    r.len = static_cast<int>(max(static_cast<int64_t>(r.len) - (hi - lo - r.n), int64_t{0}));
-  }
-  return r;
-}
-
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-
-// Two codes of a word as two bf16: those in bits 4n.. and 16 + 4n..
-template <bool kExact, int n>
-__device__ inline uint32_t pair_of(uint32_t w) {
-  if (kExact) {
-    const float lo = static_cast<float>(w >> (4 * n) & 15u), hi = static_cast<float>(w >> (16 + 4 * n) & 15u);
-    return __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, hi), __builtin_bit_cast(uint32_t, lo), 0x07060302u);
-  }
-  const uint32_t moved = n == 0 ? w << 3 : w >> (4 * n - 3);
-  // (one instruction, which takes a single constant from a scalar register: the mask stands in a vector register)
-  uint32_t r;
-  asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(r) : "v"(moved), "v"(0x00780078u), "s"(0x3F803F80u));
-  return r;
-}
-template <bool kExact>
-__device__ inline bf16x8 keys_of(uint32_t w) {
-  const u32x4 r = {pair_of<kExact, 0>(w), pair_of<kExact, 1>(w), pair_of<kExact, 2>(w), pair_of<kExact, 3>(w)};
-  return __builtin_bit_cast(bf16x8, r);
-}
-// columns 2 * half and 2 * half + 1 of a V word of both blocks: tokens (0, 2), (1, 3) of either
-template <bool kExact, int odd>
-__device__ inline bf16x8 values_of(uint32_t w0, uint32_t w1) {
-  const u32x4 r = {pair_of<kExact, odd>(w0), pair_of<kExact, 2 + odd>(w0), pair_of<kExact, odd>(w1), pair_of<kExact, 2 + odd>(w1)};
-  return __builtin_bit_cast(bf16x8, r);
-}
 
 template <int kParts>
 struct Parts {
@@ -124,21 +53,20 @@ __device__ inline Parts<kParts> split_parts(f32x8 x) {
 // Narrow (head_dim 128, up to eight rows): the eight rows stand in the columns twice, the lower eight columns work on the
 // first group of 64 values, the upper eight on the second.  A lane then reads, unpacks and applies the pairs of one group
 // only, and what it lacks of a score is in the lane eight further: 270 instead of 400 vector instructions a unit.
-template <typename T, int D, bool kNarrow_, int kTiles_>
+template <typename T, int D, bool kNarrow_>
 struct Shape {
   using Type = T;
   using B = Block<T, D>;
   static constexpr int kDim = D;
   static constexpr bool kNarrow = kNarrow_;
-  static constexpr int kTiles = kTiles_;  // column tiles of a wavefront
   static constexpr bool kExact = std::is_same<T, float>::value;
   static constexpr int kParts = kExact ? 3 : 1;
   static constexpr int kGroups = B::kGroups;
   static constexpr int kLaneGroups = kNarrow ? 1 : kGroups;  // groups a lane works on
-  static constexpr int kRows = kNarrow ? 8 : 16 * kTiles;    // flattened rows of a workgroup
+  static constexpr int kRows = kNarrow ? 8 : 16;  // flattened rows of a workgroup
   static constexpr int kWords = B::kLaneBytes / 4;
   static constexpr float kCode = kExact ? 1.f : 16.f;  // what a product with the codes has to be multiplied with
-  static_assert(!kNarrow || (kGroups == 2 && !kExact && kTiles == 1), "two groups share the columns");
+  static_assert(!kNarrow || (kGroups == 2 && !kExact), "two groups share the columns");
 };
 
 // A unit in LDS: the codes of its two blocks (K, then V), then the pairs of the first block (K, V), then of the second
@@ -197,10 +125,6 @@ __device__ inline void stage_unit(const char* block0, const char* block1, int la
     load_to_lds_16B((lane < kLanes ? block0 : block1) + U::kCodes + 16 * (lane % kLanes), lds + 2 * U::kCodes);
 }
 
-__device__ inline f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
-
-constexpr float kLowest = -3e38f;  // reference point of a column that has seen nothing
-
 // State of a column tile in one wavefront
 template <typename S>
 struct Columns {
@@ -208,7 +132,7 @@ struct Columns {
   float q_sum[S::kLaneGroups];
   f32x4 o[S::kGroups][4];      // O^T: lane (column, quarter c) holds columns 64 g + 16 c + 4 r + tile of the output
   f32x4 ones[S::kLaneGroups];  // sums of the rounded weights
-  float low[S::kLaneGroups];   // sum p * (low + 8 scale), F32: sum p * low; this lane's tokens
+  float low[S::kLaneGroups];   // sum p * (low + 8 scale), this lane's tokens
   float m, l;                  // reference point (log2 units, the same in the lanes of a column), sum p of this lane's tokens
   int limit;                   // positions 0 .. limit - 1 are seen
 };
@@ -219,130 +143,139 @@ __device__ inline float other_half(float x) {
   return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(i, i, 0x128, 0xf, 0xf, true));  // rotation of the row by eight
 }
 
-// One unit of 32 tokens.  kMasked: not every token is seen by every column (or a block is missing: bit of `have`).
-template <typename S, bool kMasked>
-__device__ inline void attend_unit(Columns<S> (&tiles)[S::kTiles], const char* unit, int pos, int have, int lane, float factor) {
+// One unit of 32 tokens.  masked: not every token is seen by every column (or a block is missing: bit of `have`).
+template <typename S>
+__device__ inline void attend_unit(Columns<S>& s, const char* unit, int pos, bool masked, int have, int lane, float factor) {
   using T = typename S::Type;
   constexpr int D = S::kDim;
   typedef typename Held<T, D>::words words;
   typedef typename Held<T, D>::pairs pairs;
   const int quarter = lane >> 4, my_group = S::kNarrow ? (lane >> 3 & 1) : 0;
+  float x[2][4];
 #pragma unroll
-  for (int t = 0; t < S::kTiles; ++t) {
-    Columns<S>& s = tiles[t];
-    float x[2][4];
+  for (int b = 0; b < 2; ++b) {
+    const words k = codes_in<T, D, false>(unit, b, lane);
+    f32x4 acc[S::kLaneGroups];
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const words k = codes_in<T, D, false>(unit, b, lane);
-      f32x4 acc[S::kLaneGroups];
+    for (int g = 0; g < S::kGroups; ++g) {
+      const int lg = S::kNarrow ? 0 : g;
+      if (!S::kNarrow || g == 0) acc[lg] = f32x4{0};
+      const bf16x8 keys[2] = {keys_of<S::kExact>(k[2 * g]), keys_of<S::kExact>(k[2 * g + 1])};
+      // (the small parts first)
 #pragma unroll
-      for (int g = 0; g < S::kGroups; ++g) {
-        const int lg = S::kNarrow ? 0 : g;
-        if (!S::kNarrow || g == 0) {
-          const float start = S::kExact ? 0.f : -s.q_sum[lg];
-          acc[lg] = f32x4{start, start, start, start};
-        }
-        const bf16x8 keys[2] = {keys_of<S::kExact>(k[2 * g]), keys_of<S::kExact>(k[2 * g + 1])};
-        // (the small parts first)
+      for (int i = S::kParts - 1; i >= 0; --i)
 #pragma unroll
-        for (int i = S::kParts - 1; i >= 0; --i)
+        for (int w = 0; w < 2; ++w) acc[lg] = mfma(keys[w], s.q[g][w].p[i], acc[lg]);
+    }
+    f32x4 sum = f32x4{0};
 #pragma unroll
-          for (int w = 0; w < 2; ++w) acc[lg] = mfma(keys[w], s.q[g][w].p[i], acc[lg]);
-      }
-      f32x4 sum = f32x4{0};
-#pragma unroll
-      for (int g = 0; g < S::kLaneGroups; ++g) {
-        const pairs p = pairs_in<T, D, false>(unit, b, S::kNarrow ? my_group : g, quarter);
-        const float base = s.q_sum[g] * (1.f / S::kCode);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float low = static_cast<float>(p[2 * r + 1]);
-          sum[r] = fmaf(static_cast<float>(p[2 * r]), acc[g][r], g ? fmaf(low, base, sum[r]) : low * base);
-        }
-      }
+    for (int g = 0; g < S::kLaneGroups; ++g) {
+      const pairs p = pairs_in<T, D, false>(unit, b, S::kNarrow ? my_group : g, quarter);
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        if (S::kNarrow) sum[r] += other_half(sum[r]);
-        const bool seen = !kMasked || ((have >> b & 1) && pos + kTokens * b + 4 * quarter + r < s.limit);
-        x[b][r] = seen ? sum[r] : -INFINITY;
+        const float scale = static_cast<float>(p[2 * r]);
+        float low = static_cast<float>(p[2 * r + 1]);
+        low = fmaf(S::kExact ? 8.f : -16.f, scale, low);  // (what the codes' operands lack, or have too much)
+        sum[r] = fmaf(scale, acc[g][r], g ? fmaf(low, s.q_sum[g], sum[r]) : low * s.q_sum[g]);
       }
     }
-    float top = x[0][0];
 #pragma unroll
-    for (int i = 1; i < 8; ++i) top = fmaxf(top, x[i / 4][i % 4]);
-    top *= factor;
-    if (__any(top > s.m + kSlack)) {
-      float m = fmaxf(s.m, top);
-      m = fmaxf(m, __shfl_xor(m, 16));
-      m = fmaxf(m, __shfl_xor(m, 32));
-      const float f = __builtin_amdgcn_exp2f(s.m - m);
-      s.m = m;
-      s.l *= f;
-#pragma unroll
-      for (int g = 0; g < S::kLaneGroups; ++g) {
-        s.low[g] *= f;
-        if (!S::kExact) s.ones[g] *= f;
-      }
-#pragma unroll
-      for (int g = 0; g < S::kGroups; ++g)
-#pragma unroll
-        for (int c = 0; c < 4; ++c) s.o[g][c] *= f;
-    }
-    float p[2][4];
+    for (int r = 0; r < 4; ++r) x[b][r] = S::kNarrow ? sum[r] + other_half(sum[r]) : sum[r];
+  }
+  if (masked)
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        p[b][r] = __builtin_amdgcn_exp2f(fmaf(x[b][r], factor, -s.m));
-        s.l += p[b][r];
+        const bool seen = (have >> b & 1) && pos + kTokens * b + 4 * quarter + r < s.limit;
+        x[b][r] = seen ? x[b][r] : -INFINITY;
       }
-    Parts<S::kParts> weights[S::kLaneGroups];
+  float top = x[0][0];
+#pragma unroll
+  for (int i = 1; i < 8; ++i) top = fmaxf(top, x[i / 4][i % 4]);
+  top *= factor;
+  if (__any(top > s.m + kSlack)) {
+    float m = fmaxf(s.m, top);
+    m = fmaxf(m, __shfl_xor(m, 16));
+    m = fmaxf(m, __shfl_xor(m, 32));
+    const float f = __builtin_amdgcn_exp2f(s.m - m);
+    s.m = m;
+    s.l *= f;
 #pragma unroll
     for (int g = 0; g < S::kLaneGroups; ++g) {
-      f32x8 w;
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        const pairs vp = pairs_in<T, D, true>(unit, b, S::kNarrow ? my_group : g, quarter);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          float scaled = p[b][r] * static_cast<float>(vp[2 * r]);
-          float low = static_cast<float>(vp[2 * r + 1]);
-          if (kMasked && x[b][r] == -INFINITY) scaled = low = 0.f;  // (what is not seen may be no number)
-          w[4 * b + (r & 1) * 2 + (r >> 1)] = scaled;               // tokens (0, 2), (1, 3)
-          s.low[g] = fmaf(p[b][r], low, s.low[g]);
-          if (!S::kExact) s.low[g] = fmaf(8.f, scaled, s.low[g]);
-        }
-      }
-      weights[g] = split_parts<S::kParts>(w);
+      s.low[g] *= f;
+      if (!S::kExact) s.ones[g] *= f;
     }
-    if (!S::kExact) {
-      const u32x4 one = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
-#pragma unroll
-      for (int g = 0; g < S::kLaneGroups; ++g) s.ones[g] = mfma(__builtin_bit_cast(bf16x8, one), weights[g].p[0], s.ones[g]);
-    }
-    const words v0 = codes_in<T, D, true>(unit, 0, lane), v1 = codes_in<T, D, true>(unit, 1, lane);
 #pragma unroll
     for (int g = 0; g < S::kGroups; ++g)
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        const bf16x8 even = values_of<S::kExact, 0>(v0[2 * g + c], v1[2 * g + c]), odd = values_of<S::kExact, 1>(v0[2 * g + c], v1[2 * g + c]);
-#pragma unroll
-        for (int i = S::kParts - 1; i >= 0; --i) {
-          s.o[g][2 * c] = mfma(even, weights[S::kNarrow ? 0 : g].p[i], s.o[g][2 * c]);
-          s.o[g][2 * c + 1] = mfma(odd, weights[S::kNarrow ? 0 : g].p[i], s.o[g][2 * c + 1]);
-        }
-      }
+      for (int c = 0; c < 4; ++c) s.o[g][c] *= f;
   }
+  float p[2][4], scaled[S::kLaneGroups][2][4], low[S::kLaneGroups][2][4];
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      p[b][r] = __builtin_amdgcn_exp2f(fmaf(x[b][r], factor, -s.m));
+      s.l += p[b][r];
+    }
+#pragma unroll
+    for (int g = 0; g < S::kLaneGroups; ++g) {
+      const pairs vp = pairs_in<T, D, true>(unit, b, S::kNarrow ? my_group : g, quarter);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        scaled[g][b][r] = p[b][r] * static_cast<float>(vp[2 * r]);
+        low[g][b][r] = fmaf(8.f, scaled[g][b][r], p[b][r] * static_cast<float>(vp[2 * r + 1]));
+      }
+    }
+  }
+  if (masked)  // (the pairs of what is not seen may be no number)
+#pragma unroll
+    for (int g = 0; g < S::kLaneGroups; ++g)
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (x[b][r] == -INFINITY) scaled[g][b][r] = low[g][b][r] = 0.f;
+  Parts<S::kParts> weights[S::kLaneGroups];
+#pragma unroll
+  for (int g = 0; g < S::kLaneGroups; ++g) {
+    f32x8 w;
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        w[4 * b + (r & 1) * 2 + (r >> 1)] = scaled[g][b][r];  // tokens (0, 2), (1, 3)
+        s.low[g] += low[g][b][r];
+      }
+    weights[g] = split_parts<S::kParts>(w);
+  }
+  if (!S::kExact) {
+    const u32x4 one = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
+#pragma unroll
+    for (int g = 0; g < S::kLaneGroups; ++g) s.ones[g] = mfma(__builtin_bit_cast(bf16x8, one), weights[g].p[0], s.ones[g]);
+  }
+  const words v0 = codes_in<T, D, true>(unit, 0, lane), v1 = codes_in<T, D, true>(unit, 1, lane);
+#pragma unroll
+  for (int g = 0; g < S::kGroups; ++g)
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const bf16x8 even = values_of<S::kExact, 0>(v0[2 * g + c], v1[2 * g + c]), odd = values_of<S::kExact, 1>(v0[2 * g + c], v1[2 * g + c]);
+#pragma unroll
+      for (int i = S::kParts - 1; i >= 0; --i) {
+        s.o[g][2 * c] = mfma(even, weights[S::kNarrow ? 0 : g].p[i], s.o[g][2 * c]);
+        s.o[g][2 * c + 1] = mfma(odd, weights[S::kNarrow ? 0 : g].p[i], s.o[g][2 * c + 1]);
+      }
+    }
 }
 
-// LDS: the units of every wavefront; at the end their partial results of a tile (rows of D + 4 floats, reference points, sums)
+// LDS: the units of every wavefront; at the end their partial results (rows of D + 4 floats, reference points, sums)
 template <typename S>
 struct AttnLds {
   using U = Unit<typename S::Type, S::kDim>;
   static constexpr int kRow = S::kDim + 4;
-  static constexpr int kCols = S::kNarrow ? 8 : 16;  // rows of a tile
   static constexpr int kWave = 2 * U::kBytes;
-  static constexpr int kMerge = kWaves * kCols * (kRow + 2) * 4;
+  static constexpr int kMerge = kWaves * S::kRows * (kRow + 2) * 4;
   static constexpr int kBytes = kWaves * kWave > kMerge ? kWaves * kWave : kMerge;
   static_assert(kBytes <= 65536, "no opt-in needed");
 };
@@ -355,12 +288,12 @@ __global__ __launch_bounds__(kWaves * 64, kWavesPerSimd) void q4_attn_kernel(Q4A
   using L = AttnLds<S>;
   using U = Unit<T, D>;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
-  typedef float PartRows[L::kCols][L::kRow];
-  typedef float PartCols[L::kCols];
+  typedef float PartRows[S::kRows][L::kRow];
+  typedef float PartCols[S::kRows];
   PartRows* part_o = reinterpret_cast<PartRows*>(lds);
   PartCols* part_m = reinterpret_cast<PartCols*>(part_o + kWaves);
   PartCols* part_l = part_m + kWaves;
-  const int lane = threadIdx.x & 63, col = lane & (L::kCols - 1), quarter = lane >> 4;
+  const int lane = threadIdx.x & 63, col = lane & (S::kRows - 1), quarter = lane >> 4;
   const int my_group = S::kNarrow ? (lane >> 3 & 1) : 0;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // heads first: neighbouring workgroups go to different L2 domains, which thus get the same share of every split, and the
@@ -388,18 +321,17 @@ __global__ __launch_bounds__(kWaves * 64, kWavesPerSimd) void q4_attn_kernel(Q4A
   const int unit_end = min((key_end + kUnit - 1) / kUnit, (split + 1) * a.split_units);
   if (a.n_splits > 1 && unit_end <= split * a.split_units) return;  // (the merge asks for no such split)
 
-  Columns<S> tiles[S::kTiles];
+  Columns<S> s;
   typedef T vec __attribute__((ext_vector_type(8), aligned(16)));
-  vec raw[S::kTiles][S::kGroups][2];
-#pragma unroll
-  for (int t = 0; t < S::kTiles; ++t) {
-    const int at = row0 + 16 * t + col, flat = min(at, n_flat - 1), token = flat / a.group, hq = head * a.group + flat % a.group;
-    tiles[t].limit = at < n_flat ? behind + token + 1 : 0;
+  vec raw[S::kGroups][2];
+  {
+    const int at = row0 + col, flat = min(at, n_flat - 1), token = flat / a.group, hq = head * a.group + flat % a.group;
+    s.limit = at < n_flat ? behind + token + 1 : 0;
     const char* q = a.q + (rq.first + token) * a.q_stride + static_cast<int64_t>(hq) * D * sizeof(T);
 #pragma unroll
     for (int g = 0; g < S::kGroups; ++g)
 #pragma unroll
-      for (int w = 0; w < 2; ++w) raw[t][g][w] = *reinterpret_cast<const vec*>(q + (g * q4::kGroup + quarter * 16 + w * 8) * sizeof(T));
+      for (int w = 0; w < 2; ++w) raw[g][w] = *reinterpret_cast<const vec*>(q + (g * kGroup + quarter * 16 + w * 8) * sizeof(T));
   }
   const int n_units = unit_end > unit0 ? (unit_end - unit0 + kWaves - 1) / kWaves : 0;  // of this wavefront
   // the blocks of the next 32 units, two lanes a unit; -1: not in the cache
@@ -423,32 +355,29 @@ __global__ __launch_bounds__(kWaves * 64, kWavesPerSimd) void q4_attn_kernel(Q4A
   };
   int have = 0;
   if (n_units > 0) have = stage(0);
+  s.m = kLowest;
+  s.l = 0.f;
 #pragma unroll
-  for (int t = 0; t < S::kTiles; ++t) {
-    Columns<S>& s = tiles[t];
-    s.m = kLowest;
-    s.l = 0.f;
+  for (int g = 0; g < S::kLaneGroups; ++g) s.q_sum[g] = s.low[g] = 0.f, s.ones[g] = f32x4{0};
 #pragma unroll
-    for (int g = 0; g < S::kLaneGroups; ++g) s.q_sum[g] = s.low[g] = 0.f, s.ones[g] = f32x4{0};
+  for (int g = 0; g < S::kGroups; ++g) {
+    const int lg = S::kNarrow ? 0 : g;
 #pragma unroll
-    for (int g = 0; g < S::kGroups; ++g) {
-      const int lg = S::kNarrow ? 0 : g;
+    for (int c = 0; c < 4; ++c) s.o[g][c] = f32x4{0};
 #pragma unroll
-      for (int c = 0; c < 4; ++c) s.o[g][c] = f32x4{0};
+    for (int w = 0; w < 2; ++w) {
+      f32x8 x = __builtin_convertvector(raw[g][w], f32x8);
+      if (S::kNarrow && g != my_group) x = f32x8{0};
+      s.q[g][w] = split_parts<S::kParts>(x);
 #pragma unroll
-      for (int w = 0; w < 2; ++w) {
-        f32x8 x = __builtin_convertvector(raw[t][g][w], f32x8);
-        if (S::kNarrow && g != my_group) x = f32x8{0};
-        s.q[g][w] = split_parts<S::kParts>(x);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) s.q_sum[lg] += x[e];
-      }
+      for (int e = 0; e < 8; ++e) s.q_sum[lg] += x[e];
     }
+  }
 #pragma unroll
-    for (int g = 0; g < S::kLaneGroups; ++g) {
-      s.q_sum[g] += __shfl_xor(s.q_sum[g], 16);
-      s.q_sum[g] += __shfl_xor(s.q_sum[g], 32);
-    }
+  for (int g = 0; g < S::kLaneGroups; ++g) {
+    s.q_sum[g] += __shfl_xor(s.q_sum[g], 16);
+    s.q_sum[g] += __shfl_xor(s.q_sum[g], 32);
+    s.q_sum[g] *= 1.f / S::kCode;
   }
   const float factor = a.scale_log2 * S::kCode;
   for (int i = 0; i < n_units; ++i) {
@@ -462,88 +391,81 @@ __global__ __launch_bounds__(kWaves * 64, kWavesPerSimd) void q4_attn_kernel(Q4A
     asm volatile("" ::: "memory");
     const char* unit = ring + (i & 1) * U::kBytes;
     const int pos = (unit0 + i * kWaves) * kUnit;
-    if (have == 3 && pos + kUnit <= key_all)
-      attend_unit<S, false>(tiles, unit, pos, have, lane, factor);
-    else
-      attend_unit<S, true>(tiles, unit, pos, have, lane, factor);
+    attend_unit(s, unit, pos, have != 3 || pos + kUnit > key_all, have, lane, factor);
     have = have_next;
   }
 
+  __syncthreads();  // (the ring has been read)
+  s.l += __shfl_xor(s.l, 16);
+  s.l += __shfl_xor(s.l, 32);
+  if (lane < S::kRows) {
+    part_m[wave][col] = s.m;
+    part_l[wave][col] = s.l;
+  }
 #pragma unroll
-  for (int t = 0; t < S::kTiles; ++t) {
-    Columns<S>& s = tiles[t];
-    __syncthreads();  // (the ring, or the tile before, has been read)
-    s.l += __shfl_xor(s.l, 16);
-    s.l += __shfl_xor(s.l, 32);
-    if (lane < L::kCols) {
-      part_m[wave][col] = s.m;
-      part_l[wave][col] = s.l;
-    }
+  for (int g = 0; g < S::kLaneGroups; ++g) {
+    s.low[g] += __shfl_xor(s.low[g], 16);
+    s.low[g] += __shfl_xor(s.low[g], 32);
+    const int group = S::kNarrow ? my_group : g;
 #pragma unroll
-    for (int g = 0; g < S::kLaneGroups; ++g) {
-      s.low[g] += __shfl_xor(s.low[g], 16);
-      s.low[g] += __shfl_xor(s.low[g], 32);
-      const int group = S::kNarrow ? my_group : g;
+    for (int r = 0; r < 4; ++r) {
+      f32x4 o;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        f32x4 o;
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const float sum = S::kNarrow && my_group ? s.o[S::kGroups - 1][c][r] : s.o[g][c][r];
-          o[c] = S::kExact ? sum + s.low[g] : fmaf(fmaf(-1.5f, s.ones[g][r], sum), S::kCode, s.low[g]);
-        }
-        *reinterpret_cast<f32x4*>(&part_o[wave][col][group * q4::kGroup + quarter * 16 + 4 * r]) = o;
+      for (int c = 0; c < 4; ++c) {
+        const float sum = S::kNarrow && my_group ? s.o[S::kGroups - 1][c][r] : s.o[g][c][r];
+        o[c] = S::kExact ? sum + s.low[g] : fmaf(fmaf(-1.5f, s.ones[g][r], sum), S::kCode, s.low[g]);
       }
+      *reinterpret_cast<f32x4*>(&part_o[wave][col][group * kGroup + quarter * 16 + 4 * r]) = o;
     }
-    __syncthreads();
+  }
+  __syncthreads();
 
-    constexpr int kThreads = kWaves * 64 / L::kCols, kEach = D / kThreads;  // threads and values per row
-    typedef float each __attribute__((ext_vector_type(kEach)));
-    const int c = threadIdx.x / kThreads, d0 = threadIdx.x % kThreads * kEach, at = row0 + 16 * t + c;
-    if (at < n_flat) {
-      float top = part_m[0][c];
+  constexpr int kThreads = kWaves * 64 / S::kRows, kEach = D / kThreads;  // threads and values per row
+  typedef float each __attribute__((ext_vector_type(kEach)));
+  const int c = threadIdx.x / kThreads, d0 = threadIdx.x % kThreads * kEach, at = row0 + c;
+  if (at < n_flat) {
+    float top = part_m[0][c];
 #pragma unroll
-      for (int w = 1; w < kWaves; ++w) top = fmaxf(top, part_m[w][c]);
-      float z = 0.f;
-      each o = each{0};
+    for (int w = 1; w < kWaves; ++w) top = fmaxf(top, part_m[w][c]);
+    float z = 0.f;
+    each o = each{0};
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
-        const float f = __builtin_amdgcn_exp2f(part_m[w][c] - top);
-        z = fmaf(f, part_l[w][c], z);
-        o += *reinterpret_cast<const each*>(&part_o[w][c][d0]) * f;
-      }
-      const bool none = z == 0.f;
-      const float inv = none ? 0.f : 1.f / z, lse2 = none ? -INFINITY : top + log2f(z);
-      o *= inv;
-      const int64_t row = (rq.first + at / a.group) * a.n_q_heads + head * a.group + at % a.group;
-      if (a.n_splits > 1) {
-        const int64_t part = row * a.n_splits + split;
-        if (d0 == 0) a.ws_lse[part] = lse2;
-        if (!none) *reinterpret_cast<each*>(a.ws_o + part * D + d0) = o;
-      } else {
-        typedef T vec __attribute__((ext_vector_type(kEach)));
-        *reinterpret_cast<vec*>(a.out + (row * D + d0) * sizeof(T)) = __builtin_convertvector(o, vec);
-        if (a.lse && d0 == 0) a.lse[row] = lse2 * 0.6931471805599453f;
-      }
+    for (int w = 0; w < kWaves; ++w) {
+      const float f = __builtin_amdgcn_exp2f(part_m[w][c] - top);
+      z = fmaf(f, part_l[w][c], z);
+      o += *reinterpret_cast<const each*>(&part_o[w][c][d0]) * f;
+    }
+    const bool none = z == 0.f;
+    const float inv = none ? 0.f : 1.f / z, lse2 = none ? -INFINITY : top + log2f(z);
+    o *= inv;
+    const int64_t row = (rq.first + at / a.group) * a.n_q_heads + head * a.group + at % a.group;
+    if (a.n_splits > 1) {
+      const int64_t part = row * a.n_splits + split;
+      if (d0 == 0) a.ws_lse[part] = lse2;
+      if (!none) *reinterpret_cast<each*>(a.ws_o + part * D + d0) = o;
+    } else {
+      typedef T vec __attribute__((ext_vector_type(kEach)));
+      *reinterpret_cast<vec*>(a.out + (row * D + d0) * sizeof(T)) = __builtin_convertvector(o, vec);
+      if (a.lse && d0 == 0) a.lse[row] = lse2 * kLn2;
     }
   }
 }
 
-// Output rows from the partial results of their splits.  A workgroup takes a row: D / 4 threads hold four columns each, and
-// 256 / (D / 4) of them share the splits, in a fixed order.
-template <typename T, int D>
+// Output rows from the partial results of their splits: D / 4 threads hold four columns each, and kShares of them share the
+// splits, in a fixed order.
+template <typename T, int D, int kShares>
 __global__ __launch_bounds__(256) void q4_merge_kernel(Q4AttnArgs a) {
-  constexpr int kLanes = D / 4, kShares = 256 / kLanes;
-  __shared__ __attribute__((aligned(16))) float sums[kShares][D];
-  __shared__ float tops[kShares], zs[kShares];
+  constexpr int kLanes = D / 4, kRows = 256 / kLanes / kShares;
+  __shared__ __attribute__((aligned(16))) float sums[kShares][kRows][D];
+  __shared__ float tops[kShares][kRows], zs[kShares][kRows];
   const Request rq = request_of(a, blockIdx.y);
-  const int64_t i = blockIdx.x;
-  if (i >= static_cast<int64_t>(rq.n) * a.n_q_heads) return;  // (the whole workgroup)
+  const int lane = threadIdx.x % kLanes, share = threadIdx.x / kLanes % kShares, mine = threadIdx.x / kLanes / kShares;
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * kRows + mine, n_rows = static_cast<int64_t>(rq.n) * a.n_q_heads;
+  if (static_cast<int64_t>(blockIdx.x) * kRows >= n_rows) return;  // (the whole workgroup)
   const int64_t row = rq.first * a.n_q_heads + i;
-  const int lane = threadIdx.x % kLanes, share = threadIdx.x / kLanes;
   const float* part = a.ws_lse + row * a.n_splits;
   // splits that hold keys of this row
-  const int keys = max(rq.len - rq.n + static_cast<int>(i) / a.n_q_heads + 1, 0);
+  const int keys = i < n_rows ? max(rq.len - rq.n + static_cast<int>(i / a.n_q_heads) + 1, 0) : 0;
   const int n_splits = keys > 0 ? min((keys - 1) / (kUnit * a.split_units) + 1, a.n_splits) : 0;
   // eight splits at a time: their loads do not wait for each other, nor an output for the log-sum-exp that says whether it
   // was written at all
@@ -574,54 +496,72 @@ __global__ __launch_bounds__(256) void q4_merge_kernel(Q4AttnArgs a) {
       for (int e = 0; e < 4; ++e) o[e] = lse[k] == -INFINITY ? o[e] : fmaf(part_o[k][e], w, o[e]);
     }
   }
-  *reinterpret_cast<f32x4*>(&sums[share][4 * lane]) = o;
-  if (lane == 0) {
-    tops[share] = top;
-    zs[share] = z;
-  }
-  __syncthreads();
-  if (threadIdx.x >= kLanes) return;
-  top = tops[0];
+  if (kShares > 1) {
+    *reinterpret_cast<f32x4*>(&sums[share][mine][4 * lane]) = o;
+    if (lane == 0) {
+      tops[share][mine] = top;
+      zs[share][mine] = z;
+    }
+    __syncthreads();
+    if (share > 0) return;
 #pragma unroll
-  for (int k = 1; k < kShares; ++k) top = fmaxf(top, tops[k]);
-  z = 0.f;
-  o = f32x4{0};
+    for (int k = 1; k < kShares; ++k) top = fmaxf(top, tops[k][mine]);
+    z = 0.f;
+    o = f32x4{0};
 #pragma unroll
-  for (int k = 0; k < kShares; ++k) {
-    const float f = __builtin_amdgcn_exp2f(tops[k] - top);
-    z = fmaf(f, zs[k], z);
-    o += *reinterpret_cast<const f32x4*>(&sums[k][4 * lane]) * f;
+    for (int k = 0; k < kShares; ++k) {
+      const float f = __builtin_amdgcn_exp2f(tops[k][mine] - top);
+      z = fmaf(f, zs[k][mine], z);
+      o += *reinterpret_cast<const f32x4*>(&sums[k][mine][4 * lane]) * f;
+    }
   }
+  if (i >= n_rows) return;
   const float inv = z == 0.f ? 0.f : 1.f / z;
   typedef T vec __attribute__((ext_vector_type(4)));
   *reinterpret_cast<vec*>(a.out + (row * D + 4 * lane) * sizeof(T)) = __builtin_convertvector(o * inv, vec);
-  if (a.lse && lane == 0) a.lse[row] = z == 0.f ? -INFINITY : (top + log2f(z)) * 0.6931471805599453f;
+  if (a.lse && lane == 0) a.lse[row] = z == 0.f ? -INFINITY : (top + log2f(z)) * kLn2;
 }
 
-// How the keys are cut: into splits of whole units for every wavefront, so that one round of workgroups (three a compute unit) covers the chip where
-// the requests alone do not, but no less than two units a wavefront.  Lengths differ, and a launch is over when its longest
-// split is: splits are cut down to 32 units as long as that makes no more than eight rounds of them.
+// Rows of a workgroup and how the keys are cut.
+//
+// Up to 96 rows of a kv head the kernel of this file takes them, 8 or 16 a workgroup, beyond that the one for many rows (28
+// heads over 4, 4 requests of 8000 tokens: 63 rows 24 us against 30, 126 rows 37 against 36; 100 rows over 3000 tokens of 32
+// kv heads 91 against 57).
+//
+// 8 or 16 rows: splits of whole units for every wavefront, so that three workgroups a compute unit are there where the requests
+// alone do not make them (four would fit with 8 rows, but smaller splits cost more: 4 requests of 19841 tokens 18.5 us
+// against 17.6), and no less than two units a wavefront.  Lengths differ, and a launch is over when its longest split is:
+// splits are cut down to 32 units as long as that makes no more than eight rounds of them.
+// Many rows: workgroups take longer, so their rounds count (two a compute unit): the number of splits with the least rounds *
+// (units of a split + 5), 5 being what a workgroup and its share of the merge cost besides, no less than 8 units each.
 struct Cut {
   int32_t rows;  // flattened rows of a workgroup
   int32_t n_splits, split_units;
   int64_t tiles;
 };
-int32_t rows_of(const mpic_ctx* ctx, int32_t max_q) {
-  const int64_t flat = static_cast<int64_t>(max_q) * ctx->group;
-  return ctx->cfg.dtype == MPIC_BF16 && flat <= 8 ? 8 : 16;
-}
 Cut cut_of(const mpic_ctx* ctx, int32_t n_requests, int32_t max_q, int64_t max_len) {
   constexpr int64_t kRound = 768, kRounds = 8, kLeast = 2 * kWaves, kMost = 32;
-  const int64_t units = std::max<int64_t>(1, (max_len + kUnit - 1) / kUnit);
+  constexpr int64_t kManyRound = 512, kManyLeast = 8, kManyCost = 5, kManySplits = 64;
+  const int64_t units = std::max<int64_t>(1, (max_len + kUnit - 1) / kUnit), flat = static_cast<int64_t>(max_q) * ctx->group;
   Cut cut;
-  cut.rows = rows_of(ctx, max_q);
-  cut.tiles = (static_cast<int64_t>(max_q) * ctx->group + cut.rows - 1) / cut.rows;
+  cut.rows = ctx->cfg.dtype != MPIC_BF16 ? 16 : flat <= 8 ? 8 : flat <= 96 ? 16 : kManyRows;
+  cut.tiles = (flat + cut.rows - 1) / cut.rows;
   const int64_t lanes = cut.tiles * ctx->cfg.n_kv_heads * n_requests;
-  const auto units_of = [&](int64_t workgroups) {  // a split's, for that many workgroups at most
-    const int64_t splits = std::max<int64_t>(1, workgroups / lanes);
-    return ((units + splits - 1) / splits + kWaves - 1) / kWaves * kWaves;
-  };
-  const int64_t each = std::max(kLeast, std::min(units_of(kRound), std::max(kMost, units_of(kRounds * kRound))));
+  const auto units_of = [&](int64_t splits, int64_t step) { return ((units + splits - 1) / splits + step - 1) / step * step; };
+  int64_t each = 0;
+  if (cut.rows == kManyRows) {
+    int64_t best = INT64_MAX;
+    for (int64_t splits = 1; splits <= kManySplits; ++splits) {
+      const int64_t n = std::max(kManyLeast, units_of(splits, kManyUnits)), used = (units + n - 1) / n;
+      const int64_t cost = (lanes * used + kManyRound - 1) / kManyRound * (n + kManyCost);
+      if (cost >= best) continue;
+      best = cost;
+      each = n;
+    }
+  } else {
+    const auto of_rounds = [&](int64_t rounds) { return units_of(std::max<int64_t>(1, rounds * kRound / lanes), kWaves); };
+    each = std::max(kLeast, std::min(of_rounds(1), std::max(kMost, of_rounds(kRounds))));
+  }
   cut.split_units = static_cast<int32_t>(each);
   cut.n_splits = static_cast<int32_t>((units + each - 1) / each);
   return cut;
@@ -635,11 +575,23 @@ int64_t workspace_of(const mpic_ctx* ctx, const Cut& cut, int64_t n_rows) {
 }
 
 template <typename S, int kWavesPerSimd>
-void launch_q4_attn(const Q4AttnArgs& a, dim3 grid, hipStream_t stream) {
+hipError_t launch_q4_attn(const Q4AttnArgs& a, dim3 grid, hipStream_t stream) {
   hipLaunchKernelGGL((q4_attn_kernel<S, kWavesPerSimd>), grid, dim3(kWaves * 64), AttnLds<S>::kBytes, stream, a);
-  if (a.n_splits > 1)
-    hipLaunchKernelGGL((q4_merge_kernel<typename S::Type, S::kDim>), dim3(static_cast<unsigned>(a.max_q) * a.n_q_heads, grid.z), dim3(256), 0,
-                       stream, a);
+  return hipGetLastError();
+}
+template <typename T, int D>
+hipError_t launch_q4_merge(const Q4AttnArgs& a, int32_t n_requests, hipStream_t stream) {
+  // up to 16 splits: a group of threads walks them all, two batches of loads (16384 rows of 8 splits: 28 -> 10 us)
+  const auto go = [&](auto shares) {
+    constexpr int kShares = decltype(shares)::value, kRows = 256 / (D / 4) / kShares;
+    const int64_t rows = static_cast<int64_t>(a.max_q) * a.n_q_heads;
+    hipLaunchKernelGGL((q4_merge_kernel<T, D, kShares>), dim3(static_cast<unsigned>((rows + kRows - 1) / kRows), n_requests), dim3(256), 0, stream, a);
+  };
+  if (a.n_splits <= 16)
+    go(std::integral_constant<int, 1>{});
+  else
+    go(std::integral_constant<int, 8>{});
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -708,13 +660,22 @@ extern "C" int mpic_q4_attn(mpic_ctx* ctx, const void* q, int64_t q_stride, int6
   hipStream_t stream = static_cast<hipStream_t>(stream_);
   const dim3 grid(static_cast<unsigned>(cut.tiles * c.n_kv_heads), cut.n_splits, n_requests);
   if (c.dtype == MPIC_BF16 && cut.rows == 8)
-    launch_q4_attn<Shape<__bf16, 128, true, 1>, 3>(a, grid, stream);
+    MPIC_HIP(ctx, (launch_q4_attn<Shape<__bf16, 128, true>, 4>(a, grid, stream)));
+  else if (c.dtype == MPIC_BF16 && cut.rows == 16)
+    MPIC_HIP(ctx, (launch_q4_attn<Shape<__bf16, 128, false>, 3>(a, grid, stream)));
   else if (c.dtype == MPIC_BF16)
-    launch_q4_attn<Shape<__bf16, 128, false, 1>, 3>(a, grid, stream);
+    MPIC_HIP(ctx, launch_q4_attn_many(a, grid, stream));
   else if (c.head_dim == 128)
-    launch_q4_attn<Shape<float, 128, false, 1>, 2>(a, grid, stream);
+    MPIC_HIP(ctx, (launch_q4_attn<Shape<float, 128, false>, 3>(a, grid, stream)));
   else
-    launch_q4_attn<Shape<float, 64, false, 1>, 3>(a, grid, stream);
-  MPIC_HIP(ctx, hipGetLastError());
+    MPIC_HIP(ctx, (launch_q4_attn<Shape<float, 64, false>, 4>(a, grid, stream)));
+  if (a.n_splits > 1) {
+    if (c.dtype == MPIC_BF16)
+      MPIC_HIP(ctx, (launch_q4_merge<__bf16, 128>(a, n_requests, stream)));
+    else if (c.head_dim == 128)
+      MPIC_HIP(ctx, (launch_q4_merge<float, 128>(a, n_requests, stream)));
+    else
+      MPIC_HIP(ctx, (launch_q4_merge<float, 64>(a, n_requests, stream)));
+  }
   return MPIC_OK;
 }
