@@ -5,10 +5,11 @@
 //   O        = sum_j (p_j scale_j) code_j + sum_j p_j low_j          (per group of columns)
 // so both products run on the codes themselves: whole numbers below 16, exact in bf16.  A pair of codes becomes a pair of
 // bf16 with one shift and one and-or, as 1 + code / 16 (the code in the upper mantissa bits of 1.0).  The ones are taken off
-// again, in the first product by starting its accumulator at -sum(q), in the second by one more product with a matrix
-// of ones, which sums the very weights (rounded) that met the codes.  There half the range of the codes goes too, 8 * scale
-// moving to the lows with the unrounded weights: what the rounding of a weight is multiplied with is then at most
-// 8 scales, not 15, and an output is off by what rounding the weights costs over a context in bf16.
+// again: of K by (low - 16 scale) in place of low, of V by one more product with a matrix of ones, which sums the very weights
+// (rounded) that met the codes.  There half the range of the codes goes too, 8 * scale moving to the lows with the unrounded
+// weights: what the rounding of a weight to bf16 is multiplied with is then at most 8 scales, not 15, and an output is off by
+// what rounding the weights costs over a context in bf16 (two bf16 parts would end that, 24 contexts of up to 32K tokens 86
+// us against 91).
 //
 // Transposed formulation: S^T = K Q^T, O^T = V^T P^T on 16x16x32 tiles whose columns are 16 flattened rows (query, head in
 // the kv group).  A lane then holds the scores of its column for tokens 4g .. 4g + 3 of both blocks of a unit of 32 tokens,

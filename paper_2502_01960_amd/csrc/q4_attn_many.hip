@@ -5,7 +5,9 @@
 // A workgroup of four wavefronts takes 128 flattened rows (query, head in the kv group), 32 each, and walks the keys 64 at a
 // time.  Every wavefront turns one of the four blocks of 16 tokens into matrix operands for all: K codes into bf16 pairs (exact,
 // scales and lows are applied to the scores: 4 operations a score), V into its values, rounded to bf16 as they would be
-// read back (two and a half operations a value once, where scaling the weights takes 7 per row and key).  The operands
+// read back (two and a half operations a value once, where scaling the weights takes 7 per row and key).  Weights go in as two
+// bf16 parts: with V rounded too, one part (623 TFLOP/s instead of 520) makes the error 1.6 times that of rounding the
+// output, two make it 1.35, as with few rows.  The operands
 // lie in LDS in the order in which lanes fetch them, in two buffers: one barrier per 64 keys, and the codes of the next 64 are
 // loaded meanwhile.
 //
@@ -183,7 +185,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void q4_attn_many_kernel(Q4AttnArgs
             x[t][k][r] = seen ? x[t][k][r] : -INFINITY;
           }
     }
-    bf16x8 p[kRowTiles][2];
+    bf16x8 p[kRowTiles][2][2];  // weights in two parts
 #pragma unroll
     for (int t = 0; t < kRowTiles; ++t) {
       __builtin_amdgcn_sched_barrier(0);
@@ -209,7 +211,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void q4_attn_many_kernel(Q4AttnArgs
           w[i] = __builtin_amdgcn_exp2f(fmaf(x[t][2 * h + i / 4][i % 4], factor, -m[t]));
           l[t] += w[i];
         }
-        p[t][h] = __builtin_convertvector(w, bf16x8);
+        p[t][h][0] = __builtin_convertvector(w, bf16x8);
+        p[t][h][1] = __builtin_convertvector(w - __builtin_convertvector(p[t][h][0], f32x8), bf16x8);
       }
     }
 #pragma unroll
@@ -219,7 +222,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void q4_attn_many_kernel(Q4AttnArgs
         if (i % 4 == 0) __builtin_amdgcn_sched_barrier(0);
         const bf16x8 values = *reinterpret_cast<const bf16x8*>(buffer + kKeys + (h * 8 + i) * 1024 + lane * 16);
 #pragma unroll
-        for (int t = 0; t < kRowTiles; ++t) o[t][i] = mfma(values, p[t][h], o[t][i]);
+        for (int t = 0; t < kRowTiles; ++t) o[t][i] = mfma(values, p[t][h][0], mfma(values, p[t][h][1], o[t][i]));
       }
   };
 
