@@ -525,14 +525,15 @@ __global__ __launch_bounds__(256) void q4_merge_kernel(Q4AttnArgs a) {
 
 // Rows of a workgroup and how the keys are cut.
 //
-// Up to 96 rows of a kv head the kernel of this file takes them, 8 or 16 a workgroup, beyond that the one for many rows (28
-// heads over 4, 4 requests of 8000 tokens: 63 rows 24 us against 30, 126 rows 37 against 36; 100 rows over 3000 tokens of 32
-// kv heads 91 against 57).
+// Up to 128 rows of a kv head the kernel of this file takes them, 8 or 16 a workgroup, beyond that the one for many rows (28
+// heads over 4, 4 requests of 8000 tokens: 63 rows 25 us against 30, 126 rows 39 against 39; 100 rows over 3000 tokens of 32
+// kv heads 90 against 64).
 //
 // 8 or 16 rows: splits of whole units for every wavefront, so that three workgroups a compute unit are there where the requests
 // alone do not make them (four would fit with 8 rows, but smaller splits cost more: 4 requests of 19841 tokens 18.5 us
 // against 17.6), and no less than two units a wavefront.  Lengths differ, and a launch is over when its longest split is:
-// splits are cut down to 32 units as long as that makes no more than eight rounds of them.
+// splits are cut down to 32 units as long as that makes no more than eight rounds of them.  Five units a wavefront stay in one
+// piece: a further unit takes 0.9 us (4 requests of 128 tokens 4.5 us, of 256 5.4), the merge 2.7 and its launch 2.3 of the host.
 // Many rows: workgroups take longer, so their rounds count (two a compute unit): the number of splits with the least rounds *
 // (units of a split + 5), 5 being what a workgroup and its share of the merge cost besides, no less than 8 units each.
 struct Cut {
@@ -541,11 +542,11 @@ struct Cut {
   int64_t tiles;
 };
 Cut cut_of(const mpic_ctx* ctx, int32_t n_requests, int32_t max_q, int64_t max_len) {
-  constexpr int64_t kRound = 768, kRounds = 8, kLeast = 2 * kWaves, kMost = 32;
+  constexpr int64_t kRound = 768, kRounds = 8, kWhole = 5 * kWaves, kLeast = 2 * kWaves, kMost = 32;
   constexpr int64_t kManyRound = 512, kManyLeast = 8, kManyCost = 5, kManySplits = 64;
   const int64_t units = std::max<int64_t>(1, (max_len + kUnit - 1) / kUnit), flat = static_cast<int64_t>(max_q) * ctx->group;
   Cut cut;
-  cut.rows = ctx->cfg.dtype != MPIC_BF16 ? 16 : flat <= 8 ? 8 : flat <= 96 ? 16 : kManyRows;
+  cut.rows = ctx->cfg.dtype != MPIC_BF16 ? 16 : flat <= 8 ? 8 : flat <= 128 ? 16 : kManyRows;
   cut.tiles = (flat + cut.rows - 1) / cut.rows;
   const int64_t lanes = cut.tiles * ctx->cfg.n_kv_heads * n_requests;
   const auto units_of = [&](int64_t splits, int64_t step) { return ((units + splits - 1) / splits + step - 1) / step * step; };
@@ -561,7 +562,7 @@ Cut cut_of(const mpic_ctx* ctx, int32_t n_requests, int32_t max_q, int64_t max_l
     }
   } else {
     const auto of_rounds = [&](int64_t rounds) { return units_of(std::max<int64_t>(1, rounds * kRound / lanes), kWaves); };
-    each = std::max(kLeast, std::min(of_rounds(1), std::max(kMost, of_rounds(kRounds))));
+    each = units <= kWhole ? kWhole : std::max(kLeast, std::min(of_rounds(1), std::max(kMost, of_rounds(kRounds))));
   }
   cut.split_units = static_cast<int32_t>(each);
   cut.n_splits = static_cast<int32_t>((units + each - 1) / each);
@@ -582,14 +583,17 @@ hipError_t launch_q4_attn(const Q4AttnArgs& a, dim3 grid, hipStream_t stream) {
 }
 template <typename T, int D>
 hipError_t launch_q4_merge(const Q4AttnArgs& a, int32_t n_requests, hipStream_t stream) {
-  // up to 16 splits: a group of threads walks them all, two batches of loads (16384 rows of 8 splits: 28 -> 10 us)
+  // a group of threads walks eight splits with one batch of loads: up to 8 splits one group a row, up to 16 two, then eight
+  // (16384 rows of 8 splits: 28 us with eight groups a row, 10 with one)
   const auto go = [&](auto shares) {
     constexpr int kShares = decltype(shares)::value, kRows = 256 / (D / 4) / kShares;
     const int64_t rows = static_cast<int64_t>(a.max_q) * a.n_q_heads;
     hipLaunchKernelGGL((q4_merge_kernel<T, D, kShares>), dim3(static_cast<unsigned>((rows + kRows - 1) / kRows), n_requests), dim3(256), 0, stream, a);
   };
-  if (a.n_splits <= 16)
+  if (a.n_splits <= 8)
     go(std::integral_constant<int, 1>{});
+  else if (a.n_splits <= 16)
+    go(std::integral_constant<int, 2>{});
   else
     go(std::integral_constant<int, 8>{});
   return hipGetLastError();

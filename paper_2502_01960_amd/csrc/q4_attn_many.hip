@@ -144,7 +144,6 @@ __global__ __launch_bounds__(kWaves * 64, 2) void q4_attn_many_kernel(Q4AttnArgs
     float x[kRowTiles][kWaves][4];
 #pragma unroll
     for (int k = 0; k < kWaves; ++k) {
-      __builtin_amdgcn_sched_barrier(0);  // (a block after the other: registers)
       bf16x8 keys[4];
       float scale[2][4], low[2][4];
 #pragma unroll
@@ -188,7 +187,6 @@ __global__ __launch_bounds__(kWaves * 64, 2) void q4_attn_many_kernel(Q4AttnArgs
     bf16x8 p[kRowTiles][2][2];  // weights in two parts
 #pragma unroll
     for (int t = 0; t < kRowTiles; ++t) {
-      __builtin_amdgcn_sched_barrier(0);
       float top = x[t][0][0];
 #pragma unroll
       for (int i = 1; i < 4 * kWaves; ++i) top = fmaxf(top, x[t][i / 4][i % 4]);
@@ -219,7 +217,6 @@ __global__ __launch_bounds__(kWaves * 64, 2) void q4_attn_many_kernel(Q4AttnArgs
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        if (i % 4 == 0) __builtin_amdgcn_sched_barrier(0);
         const bf16x8 values = *reinterpret_cast<const bf16x8*>(buffer + kKeys + (h * 8 + i) * 1024 + lane * 16);
 #pragma unroll
         for (int t = 0; t < kRowTiles; ++t) o[t][i] = mfma(values, p[t][h][0], mfma(values, p[t][h][1], o[t][i]));

@@ -236,11 +236,11 @@ class Held:
         step = max([float(np.nanmax(h[2])) for h in held[0] if h[2].size] + [0.0])
         score = 2.0 ** -21 * scale * 32 * step * np.abs(q).sum(-1, keepdims=True)
         top = max([float(np.abs(h[0]).max()) for h in held[1] if h[0].size] + [0.0])
-        # Weights times a scale of V are rounded once (bf16 2^-8) and meet codes up to 8 from the middle; where more than 96 rows of
+        # Weights times a scale of V are rounded once (bf16 2^-8) and meet codes up to 8 from the middle; where more than 128 rows of
         # a kv head are attended together V is rounded instead and the weights have 16 bits; f32: three parts, 24 bits, codes
         # up to 8 from the middle.
         step_v = max([float(h[2].max()) for h in held[1] if h[2].size] + [0.0])
-        many = max(self.news) * self.q.shape[1] // self.k[0].shape[1] > 96
+        many = max(self.news) * self.q.shape[1] // self.k[0].shape[1] > 128
         inner = 2.0 ** -22 * 8 * step_v if not self.bf16 else (2.0 ** -8 + 2.0 ** -16) * top if many else 2.0 ** -8 * 8 * step_v
         tol = 2 * score * top + inner + (2.0 ** -8 if self.bf16 else 2.0 ** -22) * np.abs(ref)
         err = np.abs(out - ref)
