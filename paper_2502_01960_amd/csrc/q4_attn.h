@@ -16,6 +16,9 @@ constexpr float kSlack = 8.0f;       // a column's reference point may lag behin
 constexpr float kLowest = -3e38f;    // reference point of a column that has seen nothing
 constexpr float kLn2 = 0.6931471805599453f;
 
+// s_waitcnt lgkmcnt(0) only
+#define MPIC_WAIT_LGKMCNT0() __builtin_amdgcn_s_waitcnt(0xC07F)
+
 struct Q4AttnArgs {
   const char* q;
   const char* cache;

@@ -383,6 +383,9 @@ __global__ __launch_bounds__(kWaves * 64, kWavesPerSimd) void q4_attn_kernel(Q4A
   const float factor = a.scale_log2 * S::kCode;
   for (int i = 0; i < n_units; ++i) {
     int have_next = 0;
+    // what was read of the half that is loaded next has arrived (all of it has been used, but nothing else orders the two)
+    MPIC_WAIT_LGKMCNT0();
+    asm volatile("" ::: "memory");
     if (i + 1 < n_units) {
       have_next = stage(i + 1);
       MPIC_WAIT_VMCNT(U::kLoads);
@@ -422,7 +425,7 @@ __global__ __launch_bounds__(kWaves * 64, kWavesPerSimd) void q4_attn_kernel(Q4A
   __syncthreads();
 
   constexpr int kThreads = kWaves * 64 / S::kRows, kEach = D / kThreads;  // threads and values per row
-  typedef float each __attribute__((ext_vector_type(kEach)));
+  typedef float each __attribute__((ext_vector_type(kEach), aligned(16)));
   const int c = threadIdx.x / kThreads, d0 = threadIdx.x % kThreads * kEach, at = row0 + c;
   if (at < n_flat) {
     float top = part_m[0][c];
@@ -445,7 +448,7 @@ __global__ __launch_bounds__(kWaves * 64, kWavesPerSimd) void q4_attn_kernel(Q4A
       if (d0 == 0) a.ws_lse[part] = lse2;
       if (!none) *reinterpret_cast<each*>(a.ws_o + part * D + d0) = o;
     } else {
-      typedef T vec __attribute__((ext_vector_type(kEach)));
+      typedef T vec __attribute__((ext_vector_type(kEach), aligned(8)));
       *reinterpret_cast<vec*>(a.out + (row * D + d0) * sizeof(T)) = __builtin_convertvector(o, vec);
       if (a.lse && d0 == 0) a.lse[row] = lse2 * kLn2;
     }
@@ -552,10 +555,10 @@ Cut cut_of(const mpic_ctx* ctx, int32_t n_requests, int32_t max_q, int64_t max_l
   const auto units_of = [&](int64_t splits, int64_t step) { return ((units + splits - 1) / splits + step - 1) / step * step; };
   int64_t each = 0;
   if (cut.rows == kManyRows) {
-    int64_t best = INT64_MAX;
+    double best = INFINITY;
     for (int64_t splits = 1; splits <= kManySplits; ++splits) {
       const int64_t n = std::max(kManyLeast, units_of(splits, kManyUnits)), used = (units + n - 1) / n;
-      const int64_t cost = (lanes * used + kManyRound - 1) / kManyRound * (n + kManyCost);
+      const double cost = static_cast<double>((lanes * used + kManyRound - 1) / kManyRound) * (n + kManyCost);
       if (cost >= best) continue;
       best = cost;
       each = n;
@@ -571,6 +574,12 @@ Cut cut_of(const mpic_ctx* ctx, int32_t n_requests, int32_t max_q, int64_t max_l
 bool sizes_fit(const mpic_ctx* ctx, int32_t n_requests, int64_t n_rows, int32_t max_q, int64_t max_len) {
   return n_requests >= 0 && n_rows >= 0 && max_q >= 1 && max_len >= 0 && n_rows < INT32_MAX && max_len <= INT32_MAX - 64 &&
          static_cast<int64_t>(max_q) * ctx->group < INT32_MAX - 256;
+}
+// The grids of both launches hold them
+bool launch_fits(const mpic_ctx* ctx, int32_t n_requests, int32_t max_q) {
+  const int64_t tiles = (static_cast<int64_t>(max_q) * ctx->group + 7) / 8;
+  return tiles * ctx->cfg.n_kv_heads <= INT32_MAX / (kWaves * 64) && static_cast<int64_t>(max_q) * ctx->cfg.n_q_heads <= INT32_MAX / 256 &&
+         n_requests <= 65535;
 }
 int64_t workspace_of(const mpic_ctx* ctx, const Cut& cut, int64_t n_rows) {
   return cut.n_splits > 1 ? n_rows * ctx->cfg.n_q_heads * cut.n_splits * (ctx->cfg.head_dim + 1) * 4 : 0;
@@ -605,6 +614,7 @@ hipError_t launch_q4_merge(const Q4AttnArgs& a, int32_t n_requests, hipStream_t 
 extern "C" int mpic_q4_attn_workspace(const mpic_ctx* ctx, int32_t n_requests, int64_t n_rows, int32_t max_q, int64_t max_len,
                                       int64_t* bytes) {
   if (!ctx || !bytes || !mpic::sizes_fit(ctx, n_requests, n_rows, max_q, max_len)) return MPIC_ERR_INVALID;
+  if (!mpic::launch_fits(ctx, n_requests, max_q)) return MPIC_ERR_UNSUPPORTED;
   *bytes = n_requests == 0 ? 0 : mpic::workspace_of(ctx, mpic::cut_of(ctx, n_requests, max_q, max_len), n_rows);
   return MPIC_OK;
 }
@@ -633,10 +643,10 @@ extern "C" int mpic_q4_attn(mpic_ctx* ctx, const void* q, int64_t q_stride, int6
   if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(cache) | reinterpret_cast<uintptr_t>(out) |
        reinterpret_cast<uintptr_t>(workspace)) & 15)
     return invalid("q4_attn: buffers must be 16-byte aligned");
+  if (!launch_fits(ctx, n_requests, max_q))
+    return fail(ctx, MPIC_ERR_UNSUPPORTED, "q4_attn: too many queries, heads or requests for one launch");
   const Cut cut = cut_of(ctx, n_requests, max_q, max_len);
   if (workspace_of(ctx, cut, n_rows) > (workspace ? workspace_bytes : 0)) return invalid("q4_attn: workspace too small");
-  if (cut.tiles * c.n_kv_heads > INT32_MAX / (kWaves * 64) || static_cast<int64_t>(max_q) * c.n_q_heads > INT32_MAX / 256 || n_requests > 65535)
-    return fail(ctx, MPIC_ERR_UNSUPPORTED, "q4_attn: too many queries, heads or requests for one launch");
   const int rc = bind_device(ctx);
   if (rc != MPIC_OK) return rc;
   Q4AttnArgs a{};

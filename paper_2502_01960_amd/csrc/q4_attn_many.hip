@@ -11,8 +11,9 @@
 // lie in LDS in the order in which lanes fetch them, in two buffers: one barrier per 64 keys, and the codes of the next 64 are
 // loaded meanwhile.
 //
-// A token whose V holds what is no number is made one whose score is no number, and its V zero: in the products a weight of
-// zero would not keep it from rows that do not see it.
+// A token whose V holds what is no number (or reaches the end of the range) is made one whose score is no number, and its V zero:
+// in the products a weight of zero would not keep it from rows that do not see it.  Slots that were never written may hold
+// anything; they are treated the same, and no row sees their scores.
 #include "q4_attn.h"
 
 namespace mpic {
@@ -32,6 +33,9 @@ constexpr int kBuffer = 2 * kKeys + kWaves * B::kPairs;
 constexpr int kLds = 2 * kBuffer;
 
 typedef __bf16 pairs8 __attribute__((ext_vector_type(8)));
+
+// Do the values of a group fit bf16?  (false also where one of the two is no number)
+__device__ inline bool in_range(float scale, float low) { return fabsf(low) + 16.f * fabsf(scale) < 3.38e38f; }
 
 // A block in registers of the wavefront that prepares it
 struct Raw {
@@ -112,7 +116,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void q4_attn_many_kernel(Q4AttnArgs
   const auto prepare = [&](const Raw& r, char* buffer) {
 #pragma unroll
     for (int w = 0; w < 4; ++w) *reinterpret_cast<bf16x8*>(buffer + (wave * 4 + w) * 1024 + lane * 16) = keys_of<false>(r.k[w]);
-    // (a block that is not in the cache is not seen: its scores are masked, and what block 0 holds in its place is finite or zeroed)
+    // (of a block that is not in the cache block 0 stands here; its scores are masked)
     char* values = buffer + kKeys + (wave >> 1) * 8 * 1024 + lane * 16 + (wave & 1) * 8;
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
@@ -121,7 +125,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void q4_attn_many_kernel(Q4AttnArgs
       for (int i = 0; i < 4; ++i) {
         scale[i] = static_cast<float>(r.vp[g][2 * i]);
         low[i] = static_cast<float>(r.vp[g][2 * i + 1]);
-        if (scale[i] != scale[i]) scale[i] = low[i] = 0.f;
+        if (!in_range(scale[i], low[i])) scale[i] = low[i] = 0.f;
       }
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
@@ -135,7 +139,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void q4_attn_many_kernel(Q4AttnArgs
     }
     if (lane < 32) {
       // (0x7FFF in both halves is no number: the pair of a token whose V is none, in either of its groups)
-      const bool nan = (r.vp1 & 0x7FFFu) > 0x7F80u;
+      const bool nan = !in_range(__builtin_bit_cast(float, r.vp1 << 16), __builtin_bit_cast(float, r.vp1 & 0xFFFF0000u));
       const bool any = __builtin_amdgcn_ballot_w64(nan) >> (lane & 15) & 0x10001u;
       *reinterpret_cast<uint32_t*>(buffer + 2 * kKeys + wave * B::kPairs + lane * 4) = any ? 0x7FFF7FFFu : r.kp;
     }

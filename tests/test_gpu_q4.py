@@ -395,6 +395,21 @@ def test_what_is_not_finite_stays_with_those_who_see_it(model):
     assert hit[2, :per].all() and hit.sum() == per * d and np.isnan(lse).sum() == per and np.isnan(lse[2, :per]).all()
 
 
+@pytest.mark.parametrize("content", [0x7F80, 0xFF80, 0x7FC0, 0x7F7F, 0xFF7F])
+@pytest.mark.parametrize("model,new", [((8, 2, 128, True), 1), ((8, 2, 128, True), 4), ((8, 2, 128, True), 40), ((4, 4, 64, False), 3)])
+def test_slots_that_were_never_written_may_hold_anything(model, new, content):
+    """Infinities, NaN and the ends of the range in every pair behind the requests' ends and in pages of nobody."""
+    p = Held([70, 100], [new, 1], *model, page=32)
+    ref, ref_lse = p.run()
+    assert np.isfinite(ref).all()
+    p.cache.view(torch.int16)[:] = content if content < 0x8000 else content - 0x10000
+    for b in range(2):
+        j = np.arange(p.lens[b])
+        mpic.mpic_q4_write(p.ctx.handle, p.k[b].to(DEV), p.v[b].to(DEV), _i32(p.table[b, j // 32] * 32 + j % 32), p.cache, p.n_slots)
+    out, lse = p.run()
+    assert np.array_equal(out, ref) and np.array_equal(lse, ref_lse)
+
+
 def test_strided_queries():
     p = Held([100, 9], [1, 1], 8, 2, 128, True)
     ref, _ = p.run(q_off=False)

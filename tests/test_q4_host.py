@@ -113,9 +113,11 @@ def test_workspace(ctx):
     assert need(0, 0, 1, 1 << 20) == 0 and need(1, 1, 1, 0) == 0 and need(1, 1, 1, 100) == 0
     assert need(1, 1, 1, 1 << 20) > 0 and need(1, 1, 1, 1 << 20) % 4 == 0
     assert need(1, 0, 1, 1 << 20) == 0
-    for a in ((-1, 1, 1, 1), (1, -1, 1, 1), (1, 1, 0, 1), (1, 1, 1, -1), (1, 1, 1, 2 ** 31)):
-        with pytest.raises(mpic.MpicError):
+    for a, status in (((-1, 1, 1, 1), INVALID), ((1, -1, 1, 1), INVALID), ((1, 1, 0, 1), INVALID), ((1, 1, 1, -1), INVALID),
+                      ((1, 1, 1, 2 ** 31), INVALID), ((65536, 65536, 1, 100), UNSUPPORTED), ((1, 1, 1 << 24, 100), UNSUPPORTED)):
+        with pytest.raises(mpic.MpicError) as e:
             need(*a)
+        assert e.value.status == status
 
 
 def test_binding_refuses_tensors_that_do_not_fit():
