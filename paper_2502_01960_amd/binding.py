@@ -414,19 +414,17 @@ def mpic_rank_tokens(dist, n_top):
     return out
 
 
-def _row_stride(t, shape, name):
+# The calls below may take the GPU 3 to 5 us, so they look at a tensor no oftener than they have to.
+def _row_stride(t, shape):
     """Elements from one row to the next of a [rows][heads][D] tensor of that shape whose rows are contiguous."""
     row, head, one = t.stride()
-    n, heads, d = shape
-    if one != 1 or head != d:
-        raise ValueError(f"{name} must be [rows][heads][D] with contiguous rows")
-    return row if n > 1 else heads * d
+    if one != 1 or head != shape[2]:
+        raise ValueError("expected a [rows][heads][D] tensor with contiguous rows")
+    return row if shape[0] > 1 else head * shape[1]
 
 
 def _int32(t, n, name):
-    """Address of a contiguous int32 tensor of n elements (None: a null pointer)."""
-    if t is None:
-        return None
+    """Address of a contiguous int32 tensor of n elements."""
     if t.numel() != n or t.element_size() != 4 or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous int32 tensor of {n} elements")
     return t.data_ptr()
@@ -444,15 +442,17 @@ def mpic_position_rows(ctx, q, k, pos, q_out, k_out, q_weight=None, k_weight=Non
     if pair_axis is not None:
         if len(pair_axis) != qs[2] // 2:
             raise ValueError("pair_axis must name an axis for each of the D / 2 pairs")
-        keep, axis = _i32_array(pair_axis)
+        axis = (C.c_int32 * len(pair_axis))(*pair_axis)
     if eps is None:
         eps = -1.0
     elif eps < 0:
         raise ValueError("eps must not be negative")
-    _check(load_library().mpic_position_rows(
-        ctx, q.data_ptr(), _row_stride(q, qs, "q"), k.data_ptr(), _row_stride(k, ks, "k"), n, _int32(pos, n_axes * n, "pos"),
-        n_axes, axis, _ptr(q_weight), _ptr(k_weight), eps, q_out.data_ptr(), _row_stride(q_out, qs, "q_out"), k_out.data_ptr(),
-        _row_stride(k_out, ks, "k_out"), _stream(stream)), ctx)
+    rc = (_lib or load_library()).mpic_position_rows(
+        ctx, q.data_ptr(), _row_stride(q, qs), k.data_ptr(), _row_stride(k, ks), n, _int32(pos, n_axes * n, "pos"), n_axes, axis,
+        None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr(), eps,
+        q_out.data_ptr(), _row_stride(q_out, qs), k_out.data_ptr(), _row_stride(k_out, ks), _stream(stream))
+    if rc:
+        _check(rc, ctx)
 
 
 def mpic_q4_bytes(ctx, n_slots):
@@ -473,9 +473,12 @@ def mpic_q4_write(ctx, k, v, slots, cache, n_slots, stream=None):
     shape = k.shape
     if v.shape != shape:
         raise ValueError("k and v must have the same shape")
-    _check(load_library().mpic_q4_write(
-        ctx, k.data_ptr(), _row_stride(k, shape, "k"), v.data_ptr(), _row_stride(v, shape, "v"), shape[0],
-        _int32(slots, shape[0], "slots"), cache.data_ptr(), _cache_bytes(cache), n_slots, _stream(stream)), ctx)
+    n = shape[0]
+    rc = (_lib or load_library()).mpic_q4_write(
+        ctx, k.data_ptr(), _row_stride(k, shape), v.data_ptr(), _row_stride(v, shape), n,
+        None if slots is None else _int32(slots, n, "slots"), cache.data_ptr(), _cache_bytes(cache), n_slots, _stream(stream))
+    if rc:
+        _check(rc, ctx)
 
 
 def mpic_q4_read(ctx, cache, n_slots, slots, k, v, stream=None):
@@ -483,9 +486,12 @@ def mpic_q4_read(ctx, cache, n_slots, slots, k, v, stream=None):
     shape = k.shape
     if v.shape != shape:
         raise ValueError("k and v must have the same shape")
-    _check(load_library().mpic_q4_read(
-        ctx, cache.data_ptr(), _cache_bytes(cache), n_slots, _int32(slots, shape[0], "slots"), shape[0], k.data_ptr(),
-        _row_stride(k, shape, "k"), v.data_ptr(), _row_stride(v, shape, "v"), _stream(stream)), ctx)
+    n = shape[0]
+    rc = (_lib or load_library()).mpic_q4_read(
+        ctx, cache.data_ptr(), _cache_bytes(cache), n_slots, None if slots is None else _int32(slots, n, "slots"), n, k.data_ptr(),
+        _row_stride(k, shape), v.data_ptr(), _row_stride(v, shape), _stream(stream))
+    if rc:
+        _check(rc, ctx)
 
 
 def mpic_q4_attn_workspace(ctx, n_requests, n_rows, max_q, max_len):
@@ -501,15 +507,19 @@ def mpic_q4_attn(ctx, q, cache, n_slots, page_table, page_size, lens, softmax_sc
     several queries per request q_off [B + 1]; all of them int32 device tensors.  workspace: a device tensor of
     mpic_q4_attn_workspace bytes."""
     shape, (b, width) = q.shape, page_table.shape
+    n = shape[0]
     if out.shape != shape or not out.is_contiguous():
         raise ValueError("out must be contiguous and like q")
-    if lse is not None and (lse.numel() != shape[0] * shape[1] or lse.element_size() != 4 or not lse.is_contiguous()):
+    if lse is not None and (lse.numel() != n * shape[1] or lse.element_size() != 4 or not lse.is_contiguous()):
         raise ValueError("lse must be a contiguous float32 [n_rows][Hq] tensor")
-    _check(load_library().mpic_q4_attn(
-        ctx, q.data_ptr(), _row_stride(q, shape, "q"), shape[0], _int32(q_off, b + 1, "q_off"), max_q, cache.data_ptr(),
-        _cache_bytes(cache), n_slots, _int32(page_table, b * width, "page_table"), width, page_size, _int32(lens, b, "lens"), b,
-        width * page_size if max_len is None else max_len, softmax_scale, out.data_ptr(), _ptr(lse), _ptr(workspace),
-        0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)), ctx)
+    rc = (_lib or load_library()).mpic_q4_attn(
+        ctx, q.data_ptr(), _row_stride(q, shape), n, None if q_off is None else _int32(q_off, b + 1, "q_off"), max_q,
+        cache.data_ptr(), _cache_bytes(cache), n_slots, _int32(page_table, b * width, "page_table"), width, page_size,
+        _int32(lens, b, "lens"), b, width * page_size if max_len is None else max_len, softmax_scale, out.data_ptr(),
+        None if lse is None else lse.data_ptr(), None if workspace is None else workspace.data_ptr(),
+        0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream))
+    if rc:
+        _check(rc, ctx)
 
 
 MPIC_TIER_MISSING, MPIC_TIER_HBM, MPIC_TIER_HOST, MPIC_TIER_DISK = 0, 1, 2, 3
