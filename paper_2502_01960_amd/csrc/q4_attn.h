@@ -30,7 +30,8 @@ struct Q4AttnArgs {
   float* ws_o;    // [rows][Hq][n_splits][D] normalised partial outputs
   float* ws_lse;  // [rows][Hq][n_splits] their log-sum-exp in log2 units, -inf: nothing seen
   int64_t n_rows, q_stride, table_width;  // q_stride in bytes
-  int32_t n_blocks, page_blocks, max_q, max_len, n_splits, split_units, n_q_heads, n_kv_heads, group;
+  int32_t n_blocks, page_blocks, max_q, max_len, n_splits, n_q_heads, n_kv_heads, group;
+  int32_t split_units, split_least, split_step;  // see units_of_split
   float scale_log2;  // softmax_scale * log2(e)
 };
 
@@ -54,6 +55,16 @@ __device__ inline Request request_of(const Q4AttnArgs& a, int b) {
     r.len = static_cast<int>(max(static_cast<int64_t>(r.len) - (hi - lo - r.n), int64_t{0}));
   }
   return r;
+}
+
+// Units of a request's splits.  In launches of many rows that are one round of workgroups a shorter request has shorter
+// splits, as many as the longest one where split_least and whole steps allow it: all end about together.  Otherwise
+// (split_least = 0) all splits are as long, and shorter requests have fewer; with few rows the first table entries are asked for
+// before the length is known.
+__device__ inline int units_of_split(const Q4AttnArgs& a, const Request& r) {
+  if (a.split_least == 0) return a.split_units;
+  const int units = (r.len + kUnit - 1) / kUnit, each = (units + a.n_splits - 1) / a.n_splits;
+  return max((each + a.split_step - 1) / a.split_step * a.split_step, a.split_least);
 }
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -86,7 +97,7 @@ __device__ inline bf16x8 values_of(uint32_t w0, uint32_t w1) {
 
 __device__ inline f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
-// Many rows per kv head (bf16): a launch whose workgroups take kManyRows flattened rows each; a.split_units is a multiple of
+// Many rows per kv head (bf16): a launch whose workgroups take kManyRows flattened rows each; splits are multiples of
 // kManyUnits units.
 constexpr int kManyRows = 128;
 constexpr int kManyUnits = 2;

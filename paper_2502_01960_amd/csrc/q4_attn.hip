@@ -470,7 +470,7 @@ __global__ __launch_bounds__(256) void q4_merge_kernel(Q4AttnArgs a) {
   const float* part = a.ws_lse + row * a.n_splits;
   // splits that hold keys of this row
   const int keys = i < n_rows ? max(rq.len - rq.n + static_cast<int>(i / a.n_q_heads) + 1, 0) : 0;
-  const int n_splits = keys > 0 ? min((keys - 1) / (kUnit * a.split_units) + 1, a.n_splits) : 0;
+  const int n_splits = keys > 0 ? min(((keys - 1) / kUnit) / units_of_split(a, rq) + 1, a.n_splits) : 0;
   // eight splits at a time: their loads do not wait for each other, nor an output for the log-sum-exp that says whether it
   // was written at all
   constexpr int kBatch = 8;
@@ -541,14 +541,14 @@ __global__ __launch_bounds__(256) void q4_merge_kernel(Q4AttnArgs a) {
 // (units of a split + 5), 5 being what a workgroup and its share of the merge cost besides, no less than 8 units each.
 struct Cut {
   int32_t rows;  // flattened rows of a workgroup
-  int32_t n_splits, split_units;
+  int32_t n_splits, split_units, split_least;  // (see units_of_split)
   int64_t tiles;
 };
 Cut cut_of(const mpic_ctx* ctx, int32_t n_requests, int32_t max_q, int64_t max_len) {
   constexpr int64_t kRound = 768, kRounds = 8, kWhole = 5 * kWaves, kLeast = 2 * kWaves, kMost = 32;
   constexpr int64_t kManyRound = 512, kManyLeast = 8, kManyCost = 5, kManySplits = 64;
   const int64_t units = std::max<int64_t>(1, (max_len + kUnit - 1) / kUnit), flat = static_cast<int64_t>(max_q) * ctx->group;
-  Cut cut;
+  Cut cut{};
   cut.rows = ctx->cfg.dtype != MPIC_BF16 ? 16 : flat <= 8 ? 8 : flat <= 128 ? 16 : kManyRows;
   cut.tiles = (flat + cut.rows - 1) / cut.rows;
   const int64_t lanes = cut.tiles * ctx->cfg.n_kv_heads * n_requests;
@@ -563,6 +563,7 @@ Cut cut_of(const mpic_ctx* ctx, int32_t n_requests, int32_t max_q, int64_t max_l
       best = cost;
       each = n;
     }
+    cut.split_least = lanes * ((units + each - 1) / each) <= kManyRound ? kManyLeast : 0;
   } else {
     const auto of_rounds = [&](int64_t rounds) { return units_of(std::max<int64_t>(1, rounds * kRound / lanes), kWaves); };
     each = units <= kWhole ? kWhole : std::max(kLeast, std::min(of_rounds(1), std::max(kMost, of_rounds(kRounds))));
@@ -668,6 +669,8 @@ extern "C" int mpic_q4_attn(mpic_ctx* ctx, const void* q, int64_t q_stride, int6
   a.max_len = static_cast<int32_t>(max_len);
   a.n_splits = cut.n_splits;
   a.split_units = cut.split_units;
+  a.split_least = cut.split_least;
+  a.split_step = kManyUnits;
   a.n_q_heads = c.n_q_heads;
   a.n_kv_heads = c.n_kv_heads;
   a.group = ctx->group;

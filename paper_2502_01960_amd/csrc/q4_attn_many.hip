@@ -56,8 +56,9 @@ __global__ __launch_bounds__(kWaves * 64, 2) void q4_attn_many_kernel(Q4AttnArgs
   if (row0 >= n_flat) return;
   const int behind = rq.len - rq.n;
   const int key_end = max(behind + (min(row0 + kManyRows, n_flat) - 1) / a.group + 1, 0);  // of the workgroup
-  const int first = split * a.split_units * kUnit;                                       // keys of the split
-  const int end = min(key_end, first + a.split_units * kUnit);
+  const int64_t each = static_cast<int64_t>(units_of_split(a, rq)) * kUnit;
+  const int64_t from = split * each;  // keys of the split
+  const int first = static_cast<int>(min(from, static_cast<int64_t>(key_end))), end = static_cast<int>(min(from + each, static_cast<int64_t>(key_end)));
   if (a.n_splits > 1 && end <= first) return;  // (the merge asks for no such split)
   const int n_steps = end > first ? (end - first + kStep - 1) / kStep : 0;
   // of this wavefront: rows, keys that some of them see, keys that all of them see
@@ -97,12 +98,22 @@ __global__ __launch_bounds__(kWaves * 64, 2) void q4_attn_many_kernel(Q4AttnArgs
   const float factor = a.scale_log2 * 16.f;
 
   const int32_t* table = a.table + b * a.table_width;
+  // blocks of this wavefront's next 64 steps, one a lane; -1: not in the cache
+  int ids = -1;
+  const auto look_up = [&](int step0) {
+    const int64_t block = first / kTokens + static_cast<int64_t>(step0 + lane) * kWaves + wave;
+    ids = -1;
+    if (block * kTokens < end) {
+      const int n = static_cast<int>(block);
+      const int64_t id = static_cast<int64_t>(table[n / a.page_blocks]) * a.page_blocks + n % a.page_blocks;
+      if (id >= 0 && id < a.n_blocks) ids = static_cast<int>(id);
+    }
+  };
   const auto load = [&](int step) {
     Raw r;
-    const int block = first / kTokens + step * kWaves + wave;
-    int64_t id = -1;
-    if (block * kTokens < end) id = static_cast<int64_t>(table[block / a.page_blocks]) * a.page_blocks + block % a.page_blocks;
-    r.have = id >= 0 && id < a.n_blocks;
+    if ((step & 63) == 0) look_up(step);
+    const int64_t id = __builtin_amdgcn_readlane(ids, step & 63);
+    r.have = id >= 0;
     const char* p = a.cache + ((r.have ? id : 0) * a.n_kv_heads + head) * B::kBytes;
     r.k = *reinterpret_cast<const u32x4*>(p + lane * 16);
     r.v = *reinterpret_cast<const u32x4*>(p + B::kV + lane * 16);
