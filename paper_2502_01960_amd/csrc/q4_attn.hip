@@ -528,9 +528,12 @@ __global__ __launch_bounds__(256) void q4_merge_kernel(Q4AttnArgs a) {
 
 // Rows of a workgroup and how the keys are cut.
 //
-// Up to 128 rows of a kv head the kernel of this file takes them, 8 or 16 a workgroup, beyond that the one for many rows (28
-// heads over 4, 4 requests of 8000 tokens: 63 rows 25 us against 30, 126 rows 39 against 39; 100 rows over 3000 tokens of 32
-// kv heads 90 against 64).
+// The kernel of this file takes 8 or 16 rows a workgroup, the one for many rows 128 of them, which share what is read of the
+// keys: a fifth of the work of a workgroup of 16, but steps that are long and wait for each other.  So it takes over where the
+// launch is large enough that work counts and not the length of a step, by (tiles of 16 rows) * (units of keys) over all kv
+// heads and requests: 23 000 of them 31 us against 27 with 16 rows (28 heads over 4, 2 requests of 7300 tokens, 61 rows each),
+// 51 000 equal, 84 000 64 against 76 (100 rows over 3000 tokens of 32 kv heads), 104 000 76 against 86, and 12 % less in larger
+// ones.  Below 96 rows its tile would be half empty.
 //
 // 8 or 16 rows: splits of whole units for every wavefront, so that three workgroups a compute unit are there where the requests
 // alone do not make them (four would fit with 8 rows, but smaller splits cost more: 4 requests of 19841 tokens 18.5 us
@@ -546,10 +549,11 @@ struct Cut {
 };
 Cut cut_of(const mpic_ctx* ctx, int32_t n_requests, int32_t max_q, int64_t max_len) {
   constexpr int64_t kRound = 768, kRounds = 8, kWhole = 5 * kWaves, kLeast = 2 * kWaves, kMost = 32;
-  constexpr int64_t kManyRound = 512, kManyLeast = 8, kManyCost = 5, kManySplits = 64;
+  constexpr int64_t kFew = 96, kManyWork = 65536, kManyRound = 512, kManyLeast = 8, kManyCost = 5, kManySplits = 64;
   const int64_t units = std::max<int64_t>(1, (max_len + kUnit - 1) / kUnit), flat = static_cast<int64_t>(max_q) * ctx->group;
   Cut cut{};
-  cut.rows = ctx->cfg.dtype != MPIC_BF16 ? 16 : flat <= 8 ? 8 : flat <= 128 ? 16 : kManyRows;
+  const double work = static_cast<double>((flat + 15) / 16 * ctx->cfg.n_kv_heads) * n_requests * units;
+  cut.rows = ctx->cfg.dtype != MPIC_BF16 ? 16 : flat <= 8 ? 8 : flat <= kFew || work < kManyWork ? 16 : kManyRows;
   cut.tiles = (flat + cut.rows - 1) / cut.rows;
   const int64_t lanes = cut.tiles * ctx->cfg.n_kv_heads * n_requests;
   const auto units_of = [&](int64_t splits, int64_t step) { return ((units + splits - 1) / splits + step - 1) / step * step; };

@@ -1,6 +1,6 @@
-// Attention over contexts held in 4 bits, many rows per kv head (gfx950, bf16): the question of a next turn, a prompt in
-// chunks.  Formulas and formulation as in q4_attn.hip; other work bounds it: 4 D flops per row and key for D bytes of codes a
-// key make it a matter of the matrix cores and of the vector instructions around them.
+// Attention over contexts held in 4 bits, large launches of many rows per kv head (gfx950, bf16): a prompt in chunks, the
+// questions of a next turn over long contexts.  Formulas and formulation as in q4_attn.hip; other work bounds it: 4 D flops per
+// row and key for D bytes of codes a key make it a matter of the matrix cores and of the vector instructions around them.
 //
 // A workgroup of four wavefronts takes 128 flattened rows (query, head in the kv group), 32 each, and walks the keys 64 at a
 // time.  Every wavefront turns one of the four blocks of 16 tokens into matrix operands for all: K codes into bf16 pairs (exact,

@@ -218,9 +218,11 @@ class Held:
 
     def run(self, max_len=None, max_q=None, q_off=True, lse=True):
         q = self.q.to(DEV)
+        table = self.table if max_len is None else np.pad(self.table, ((0, 0), (0, max(0, -(-max_len // self.page) - self.table.shape[1]))),
+                                                          constant_values=-1)
         out = torch.full(self.q.shape, 77.0, dtype=_dt(self.bf16), device=DEV)
         l = torch.full(self.q.shape[:2], 77.0, dtype=torch.float32, device=DEV) if lse else None
-        _attend(self.ctx, q, self.cache, self.n_slots, _i32(self.table), self.page, _i32(self.lens), out, l,
+        _attend(self.ctx, q, self.cache, self.n_slots, _i32(table), self.page, _i32(self.lens), out, l,
                 _i32(self.q_off) if q_off else None, max_q or max(self.news + [1]) if q_off else 1, max_len)
         return out.double().cpu().numpy(), None if l is None else l.double().cpu().numpy()
 
@@ -236,12 +238,14 @@ class Held:
         step = max([float(np.nanmax(h[2])) for h in held[0] if h[2].size] + [0.0])
         score = 2.0 ** -21 * scale * 32 * step * np.abs(q).sum(-1, keepdims=True)
         top = max([float(np.abs(h[0]).max()) for h in held[1] if h[0].size] + [0.0])
-        # Weights times a scale of V are rounded once (bf16 2^-8) and meet codes up to 8 from the middle; where more than 128 rows of
-        # a kv head are attended together V is rounded instead and the weights have 16 bits; f32: three parts, 24 bits, codes
+        # Weights times a scale of V are rounded once (bf16 2^-8) and meet codes up to 8 from the middle; where more than 96 rows of
+        # a kv head are attended together V may be rounded instead and the weights have 16 bits; f32: three parts, 24 bits, codes
         # up to 8 from the middle.
         step_v = max([float(h[2].max()) for h in held[1] if h[2].size] + [0.0])
-        many = max(self.news) * self.q.shape[1] // self.k[0].shape[1] > 128
-        inner = 2.0 ** -22 * 8 * step_v if not self.bf16 else (2.0 ** -8 + 2.0 ** -16) * top if many else 2.0 ** -8 * 8 * step_v
+        many = max(self.news) * self.q.shape[1] // self.k[0].shape[1] > 96
+        inner = 2.0 ** -8 * 8 * step_v if self.bf16 else 2.0 ** -22 * 8 * step_v
+        if many and self.bf16:
+            inner = max(inner, (2.0 ** -8 + 2.0 ** -16) * top)
         tol = 2 * score * top + inner + (2.0 ** -8 if self.bf16 else 2.0 ** -22) * np.abs(ref)
         err = np.abs(out - ref)
         assert (err <= tol).all(), float((err / np.maximum(tol, 1e-30)).max())
@@ -296,30 +300,48 @@ def test_sharp_and_flat_scores(news):
     for spread in (30.0, 0.0):
         p = Held([1000, 40], news, 8, 2, 128, True, spread=spread)
         p.check(*p.run())
+        p.check(*p.run(max_len=1 << 19))
 
 
-@pytest.mark.parametrize("news", [[60], [61]])
-def test_splits_of_many_rows(news):
-    """Long enough to be cut; with and without a query per kv head that is left over."""
-    p = Held([5000], news, 8, 2, 128, True, page=64)
-    p.check(*p.run())
-    p.check(*p.run(max_len=5000))
+BOUND = 1 << 19      # a bound on the lengths that makes a launch of more than 96 rows a large one, whatever the lengths are
 
 
-def test_many_rows_and_what_is_not_finite():
-    """A value that is no number reaches the rows that see it, whole; pages of nobody and behind the end reach none."""
+@pytest.mark.parametrize("model", [m for m in MODELS if m[3]])
+@pytest.mark.parametrize("lens,news", [([200, 64], [130, 64]), ([3, 1, 0], [140, 2, 3]), ([1025, 63, 129], [1, 200, 7]), ([700, 130], [150, 130])])
+def test_large_launches_of_many_rows(model, lens, news):
+    """Few of the rows and keys that the bounds announce are there."""
+    p = Held(lens, news, *model, page=32)
+    p.check(*p.run(max_len=BOUND))
+    p.check(*p.run(max_len=BOUND, max_q=1500))
+
+
+@pytest.mark.parametrize("max_q", [None, 640])
+@pytest.mark.parametrize("news", [[60, 1], [61, 30]])
+def test_splits_of_many_rows(news, max_q):
+    """Long enough to be cut; with and without a query per kv head that is left over; one round of workgroups and several."""
+    p = Held([5000, 1111], news, 8, 2, 128, True, page=64)
+    for max_len in (None, 5000, 100000, BOUND):
+        p.check(*p.run(max_len=max_len, max_q=max_q))
+
+
+@pytest.mark.parametrize("large", [False, True])
+def test_many_rows_and_what_is_not_finite(large):
+    """A value that is no number reaches the rows that see it (whole rows in large launches); pages of nobody and behind the end
+    reach none."""
+    bound = BOUND if large else None
     p = Held([90, 70], [60, 30], 8, 2, 128, True, page=32)
-    ref, ref_lse = p.run()
+    ref, ref_lse = p.run(max_len=bound)
     v = p.v[0][50:51].clone()
     v[0, 1, 3] = float("inf")
     nan = torch.full((26, 2, 128), float("nan"), dtype=torch.bfloat16, device=DEV)
     mpic.mpic_q4_write(p.ctx.handle, nan, nan, _i32(p.table[1, 2] * 32 + np.arange(6, 32)), p.cache, p.n_slots)
     mpic.mpic_q4_write(p.ctx.handle, p.k[0][50:51].to(DEV), v.to(DEV), _i32(p.table[0, [1]] * 32 + 18), p.cache, p.n_slots)
-    out, lse = p.run()
+    out, lse = p.run(max_len=bound)
     hit = np.isnan(out)
     want = np.zeros_like(hit)
-    want[20:60, 4:] = True        # queries at positions 50 and more, heads of kv head 1
-    assert np.array_equal(hit, want) and np.array_equal(np.isnan(lse), want[..., 0])
+    want[20:60, 4:, :128 if large else 64] = True        # queries at positions 50 and more, heads of kv head 1
+    assert np.array_equal(hit, want)
+    assert np.array_equal(np.isnan(lse), want[..., 0] & large)
     assert np.array_equal(out[~want], ref[~want])
 
 
@@ -396,17 +418,18 @@ def test_what_is_not_finite_stays_with_those_who_see_it(model):
 
 
 @pytest.mark.parametrize("content", [0x7F80, 0xFF80, 0x7FC0, 0x7F7F, 0xFF7F])
-@pytest.mark.parametrize("model,new", [((8, 2, 128, True), 1), ((8, 2, 128, True), 4), ((8, 2, 128, True), 40), ((4, 4, 64, False), 3)])
-def test_slots_that_were_never_written_may_hold_anything(model, new, content):
+@pytest.mark.parametrize("model,new,bound", [((8, 2, 128, True), 1, None), ((8, 2, 128, True), 4, None), ((8, 2, 128, True), 40, None),
+                                             ((8, 2, 128, True), 40, BOUND), ((4, 4, 64, False), 3, None)])
+def test_slots_that_were_never_written_may_hold_anything(model, new, bound, content):
     """Infinities, NaN and the ends of the range in every pair behind the requests' ends and in pages of nobody."""
     p = Held([70, 100], [new, 1], *model, page=32)
-    ref, ref_lse = p.run()
+    ref, ref_lse = p.run(max_len=bound)
     assert np.isfinite(ref).all()
     p.cache.view(torch.int16)[:] = content if content < 0x8000 else content - 0x10000
     for b in range(2):
         j = np.arange(p.lens[b])
         mpic.mpic_q4_write(p.ctx.handle, p.k[b].to(DEV), p.v[b].to(DEV), _i32(p.table[b, j // 32] * 32 + j % 32), p.cache, p.n_slots)
-    out, lse = p.run()
+    out, lse = p.run(max_len=bound)
     assert np.array_equal(out, ref) and np.array_equal(lse, ref_lse)
 
 
