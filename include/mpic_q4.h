@@ -48,7 +48,7 @@ extern "C" {
  *   q_out, k_out      device, like q and k.  May be q and k themselves with the same strides;
  *                     must not overlap them otherwise
  * A row of zeros stays zeros for eps > 0; with eps = 0 it becomes NaN, as the formula says.
- * Errors: MPIC_ERR_INVALID, MPIC_ERR_HIP.
+ * Errors: MPIC_ERR_INVALID, MPIC_ERR_UNSUPPORTED (launch beyond the grid's limits), MPIC_ERR_HIP.
  */
 int mpic_position_rows(mpic_ctx* ctx, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
                        int64_t n_rows, const int32_t* pos, int32_t n_axes, const int32_t* pair_axis,
@@ -80,7 +80,7 @@ int mpic_q4_bytes(const mpic_ctx* ctx, int64_t n_slots, int64_t* bytes);
  *                     is then undefined (part of one row, part of another)
  *   cache             device, 16-byte aligned; other slots keep what they hold
  *   cache_bytes       size of the buffer, at least mpic_q4_bytes for n_slots
- * Errors: MPIC_ERR_INVALID, MPIC_ERR_HIP.
+ * Errors: MPIC_ERR_INVALID, MPIC_ERR_UNSUPPORTED (launch beyond the grid's limits), MPIC_ERR_HIP.
  */
 int mpic_q4_write(mpic_ctx* ctx, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
                   int64_t n_rows, const int32_t* slots, void* cache, int64_t cache_bytes, int64_t n_slots,
@@ -111,12 +111,13 @@ int mpic_q4_read(mpic_ctx* ctx, const void* cache, int64_t cache_bytes, int64_t 
  *
  *   q                 device [n_rows][Hq][D], rows q_stride elements apart (as above)
  *   q_off             device [n_requests + 1], queries of request b are rows q_off[b] ..
- *                     q_off[b+1]) - 1; NULL: one query per request, n_rows = n_requests.  Rows of
- *                     no request are left as they were
+ *                     q_off[b + 1] - 1 (never decreasing); NULL: one query per request, n_rows =
+ *                     n_requests.  Rows of no request are left as they were
  *   max_q             most queries of a request, >= 1 (shapes the launch; queries beyond it are
  *                     not computed)
  *   page_table        device [n_requests][table_width]; entries behind a request's last page may
- *                     hold anything.  Tokens whose page is not inside the cache are not seen
+ *                     hold anything.  Tokens whose block of 16 slots is not inside the cache are
+ *                     not seen
  *   page_size         a positive multiple of 16.  Contiguous caches are those with one page per
  *                     request
  *   lens              device [n_requests]; negative = 0, more than max_len = max_len
@@ -124,10 +125,12 @@ int mpic_q4_read(mpic_ctx* ctx, const void* cache, int64_t cache_bytes, int64_t 
  *                     the lengths makes it faster)
  *   out               device [n_rows][Hq][D]
  *   lse               device float [n_rows][Hq]; may be NULL
- *   workspace         device, 16-byte aligned, at least mpic_q4_attn_workspace bytes (may be NULL
- *                     for 0 bytes), any content.  It is the caller's so that graphs and streams
+ *   workspace         device, 16-byte aligned, at least mpic_q4_attn_workspace bytes for the same
+ *                     counts and bounds (smaller bounds may need more; may be NULL for 0 bytes), any
+ *                     content.  It is the caller's so that graphs and streams
  *                     that may run beside each other can have one each; calls that may overlap
  *                     must not share one
+ * Scores and sums are fp32: |V| up to 2^80 cannot overflow them.
  * Values that are not finite reach the queries that see them and no others, those of V only the 64
  * neighbouring columns that share their group (in large launches of more than 96 rows their whole
  * rows).

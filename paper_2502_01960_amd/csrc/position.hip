@@ -8,6 +8,8 @@
 // modulo 2^64 is the angle modulo a full turn, exact to 2^-33 of a turn for any int32 position, where an fp32 product is off
 // by 5e-3 radians at 75K tokens already.  Its two leading bits are the quadrant, the rest goes through the Taylor
 // series of sine and cosine on [-pi/4, pi/4] (next terms below 2e-9).
+#include <algorithm>
+#include <cfloat>
 #include <cmath>
 
 #include "common.h"
@@ -177,6 +179,7 @@ extern "C" int mpic_position_rows(mpic_ctx* ctx, const void* q, int64_t q_stride
     return fail(ctx, MPIC_ERR_INVALID, "position_rows: buffers must be 16-byte aligned");
   if ((q == q_out && q_stride != q_out_stride) || (k == k_out && k_stride != k_out_stride))
     return fail(ctx, MPIC_ERR_INVALID, "position_rows: rows positioned in place must keep their stride");
+  if (n_rows > INT32_MAX / 64) return fail(ctx, MPIC_ERR_UNSUPPORTED, "position_rows: too many rows for one launch");  // (threads of a launch)
   const int rc = bind_device(ctx);
   if (rc != MPIC_OK) return rc;
   if (!ctx->turns_known) {
@@ -202,7 +205,7 @@ extern "C" int mpic_position_rows(mpic_ctx* ctx, const void* q, int64_t q_stride
   a.k_out_stride = k_out_stride;
   a.n_q_heads = c.n_q_heads;
   a.n_heads = c.n_q_heads + c.n_kv_heads;
-  a.eps = static_cast<float>(eps);
+  a.eps = eps > 0 ? std::max(static_cast<float>(eps), FLT_MIN) : 0.f;  // (zeros stay zeros however small it is)
   a.n_axes = n_axes;
   hipStream_t stream = static_cast<hipStream_t>(stream_);
   const bool norm = eps >= 0, inter = c.rope_interleaved != 0;

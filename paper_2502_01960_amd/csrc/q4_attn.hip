@@ -576,8 +576,9 @@ Cut cut_of(const mpic_ctx* ctx, int32_t n_requests, int32_t max_q, int64_t max_l
   cut.n_splits = static_cast<int32_t>((units + each - 1) / each);
   return cut;
 }
+// (n_rows * n_q_heads: nothing derived from it passes 64 bits)
 bool sizes_fit(const mpic_ctx* ctx, int32_t n_requests, int64_t n_rows, int32_t max_q, int64_t max_len) {
-  return n_requests >= 0 && n_rows >= 0 && max_q >= 1 && max_len >= 0 && n_rows < INT32_MAX && max_len <= INT32_MAX - 64 &&
+  return n_requests >= 0 && n_rows >= 0 && max_q >= 1 && max_len >= 0 && n_rows < INT32_MAX && n_rows * ctx->cfg.n_q_heads < int64_t{1} << 38 && max_len <= INT32_MAX - 64 &&
          static_cast<int64_t>(max_q) * ctx->group < INT32_MAX - 256;
 }
 // The grids of both launches hold them

@@ -127,6 +127,16 @@ def test_rows_that_are_zero_or_not_finite_stay_their_own():
     assert torch.isfinite(q[[0, 3]].float()).all() and torch.isfinite(q[2, 0].float()).all() and torch.isfinite(k[:3].float()).all()
 
 
+@pytest.mark.parametrize("bf16", [True, False])
+def test_zeros_stay_zeros_for_any_eps(bf16):
+    ctx = mpic.Context(2, 1, 128, mpic.MPIC_BF16 if bf16 else mpic.MPIC_F32, 1e4)
+    for eps in (1e-300, 1e-40, 1e300):
+        q, k = (torch.zeros((3, h, 128), dtype=torch.bfloat16 if bf16 else torch.float32, device=DEV) for h in (2, 1))
+        mpic.mpic_position_rows(ctx.handle, q, k, torch.arange(3, dtype=torch.int32, device=DEV), q, k, eps=eps)
+        torch.cuda.synchronize()
+        assert (q == 0).all() and (k == 0).all(), eps
+
+
 def test_no_rows():
     ctx = mpic.Context(2, 1, 128, mpic.MPIC_BF16, 1e4)
     e = lambda h: torch.empty((0, h, 128), dtype=torch.bfloat16, device=DEV)

@@ -417,6 +417,59 @@ def test_what_is_not_finite_stays_with_those_who_see_it(model):
     assert hit[2, :per].all() and hit.sum() == per * d and np.isnan(lse).sum() == per and np.isnan(lse[2, :per]).all()
 
 
+@pytest.mark.parametrize("model,bound", [((8, 2, 128, True), None), ((28, 4, 128, True), None), ((28, 4, 128, True), BOUND), ((4, 4, 64, False), None)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_queries_that_are_not_finite_stay_alone(model, bound, bad):
+    p = Held([70, 300], [2, 25], *model, page=32)
+    ref, ref_lse = p.run(max_len=bound)
+    for row, head in ((0, 1), (26, 0), (7, 3)):
+        p.q[row, head, 5] = bad
+    out, lse = p.run(max_len=bound)
+    hit = np.zeros(ref_lse.shape, bool)
+    for row, head in ((0, 1), (26, 0), (7, 3)):
+        hit[row, head] = True
+    assert np.isnan(out[hit]).all() and np.isnan(lse[hit]).all()
+    assert np.array_equal(out[~hit], ref[~hit]) and np.array_equal(lse[~hit], ref_lse[~hit])
+
+
+@pytest.mark.parametrize("bound", [1024, BOUND])
+def test_captured_many_rows_follow_lengths_offsets_and_pages(bound):
+    """One graph per bound, replayed with other lengths, offsets and tables, against the eager call."""
+    p = Held([900, 300], [40, 25], 28, 4, 128, True, page=32)
+    width = bound // 32
+    pad = lambda t: np.pad(t, ((0, 0), (0, max(0, width - t.shape[1]))), constant_values=-1)[:, :width]
+    inputs = [([900, 300], [0, 40, 65], pad(p.table)), ([31, 0], [0, 1, 1], pad(p.table)), ([300, 900], [3, 3, 43], pad(p.table[::-1])),
+              ([512, 257], [0, 0, 40], pad(p.table))]
+    q, lens, off, table = p.q.to(DEV), _i32([0, 0]), _i32([0, 0, 0]), _i32(pad(p.table))
+    out, lse = torch.zeros_like(q), torch.zeros(q.shape[:2], device=DEV)
+    ws = torch.empty(max(1, mpic.mpic_q4_attn_workspace(p.ctx.handle, 2, 65, 40, bound)), dtype=torch.uint8, device=DEV)
+    call = lambda: mpic.mpic_q4_attn(p.ctx.handle, q, p.cache, p.n_slots, table, 32, lens, 0.1, out, lse, off, 40, bound, ws)
+
+    def feed(i):
+        lens.copy_(_i32(inputs[i][0]))
+        off.copy_(_i32(inputs[i][1]))
+        table.copy_(_i32(np.ascontiguousarray(inputs[i][2])))
+        out.fill_(7.0)
+        lse.fill_(7.0)
+
+    eager = []
+    for i in range(len(inputs)):
+        feed(i)
+        call()
+        torch.cuda.synchronize()
+        eager.append((out.clone(), lse.clone()))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for i in (0, 1, 2, 3, 2, 0):
+        feed(i)
+        ws.fill_(0xFF)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager[i][0]) and torch.equal(lse, eager[i][1]), i
+        torch.randn(1000, device=DEV).sum().item()
+
+
 @pytest.mark.parametrize("content", [0x7F80, 0xFF80, 0x7FC0, 0x7F7F, 0xFF7F])
 @pytest.mark.parametrize("model,new,bound", [((8, 2, 128, True), 1, None), ((8, 2, 128, True), 4, None), ((8, 2, 128, True), 40, None),
                                              ((8, 2, 128, True), 40, BOUND), ((4, 4, 64, False), 3, None)])

@@ -52,6 +52,7 @@ def test_position_rows_refuses(ctx):
     assert "position_rows" in mpic.binding.mpic_last_error(ctx.handle)
     assert _lib().mpic_position_rows(*([None, A, 1024, A, 256, 4, A, 1, None, None, None, 0.0, A, 1024, A, 256, None])) == INVALID
     assert _position(ctx, n=0, q=None, k=None, pos=None, qo=None, ko=None) == 0
+    assert _position(ctx, n=2 ** 31 - 2) == UNSUPPORTED
 
 
 def _write(ctx, read=False, **kw):
@@ -113,6 +114,10 @@ def test_workspace(ctx):
     assert need(0, 0, 1, 1 << 20) == 0 and need(1, 1, 1, 0) == 0 and need(1, 1, 1, 100) == 0
     assert need(1, 1, 1, 1 << 20) > 0 and need(1, 1, 1, 1 << 20) % 4 == 0
     assert need(1, 0, 1, 1 << 20) == 0
+    wide = mpic.Context(1 << 10, 1, 128, mpic.MPIC_BF16, 1e4)
+    with pytest.raises(mpic.MpicError):
+        mpic.mpic_q4_attn_workspace(wide.handle, 1, 2 ** 31 - 2, 1, 1 << 20)
+    assert mpic.mpic_q4_attn_workspace(wide.handle, 1, 1 << 20, 1, 1 << 30) > 1 << 40
     for a, status in (((-1, 1, 1, 1), INVALID), ((1, -1, 1, 1), INVALID), ((1, 1, 0, 1), INVALID), ((1, 1, 1, -1), INVALID),
                       ((1, 1, 1, 2 ** 31), INVALID), ((65536, 65536, 1, 100), UNSUPPORTED), ((1, 1, 1 << 24, 100), UNSUPPORTED)):
         with pytest.raises(mpic.MpicError) as e:
