@@ -104,10 +104,9 @@ int mpic_q4_read(mpic_ctx* ctx, const void* cache, int64_t cache_bytes, int64_t 
  * over the values that the codes stand for.  A query that sees nothing (p < 0, or an empty
  * request) gets zeros and lse = -infinity.
  * BF16: products on the matrix cores with fp32 accumulation over the codes themselves, which are
- * exact; scales and minima are applied in fp32, the weights (times the scale of V) are rounded to
- * bf16 before the second product, one final rounding of out.  Large launches of more than 96 rows
- * (max_q * Hq / Hkv) may round V to bf16 instead, as it would be read back, and use the weights as
- * two bf16 parts.  F32: factors split into three bf16 parts (24 bits), fp32 otherwise.
+ * exact; the weights (times the scale of V) are rounded to bf16 before the second product, those
+ * that meet V's minima to two bf16 parts; one final rounding of out.  F32: factors split into
+ * three bf16 parts (24 bits), fp32 otherwise.
  *
  *   q                 device [n_rows][Hq][D], rows q_stride elements apart (as above)
  *   q_off             device [n_requests + 1], queries of request b are rows q_off[b] ..
@@ -132,8 +131,7 @@ int mpic_q4_read(mpic_ctx* ctx, const void* cache, int64_t cache_bytes, int64_t 
  *                     must not share one
  * Scores and sums are fp32: |V| up to 2^80 cannot overflow them.
  * Values that are not finite reach the queries that see them and no others, those of V only the 64
- * neighbouring columns that share their group (in large launches of more than 96 rows their whole
- * rows).
+ * neighbouring columns that share their group.
  * Errors: MPIC_ERR_INVALID, MPIC_ERR_UNSUPPORTED (launch beyond the grid's limits), MPIC_ERR_HIP.
  */
 int mpic_q4_attn_workspace(const mpic_ctx* ctx, int32_t n_requests, int64_t n_rows, int32_t max_q,

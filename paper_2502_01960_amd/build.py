@@ -10,7 +10,7 @@ LIB = os.path.join(HERE, "libmpic.so")
 PROBE_LIB = os.path.join(HERE, "libmpic_probe.so")   # measurement aid (bench.py --mfma-ceiling), not part of the product library
 PROBE_SOURCES = ["probe_mfma.hip", "probe_read.hip"]
 SOURCES = ["plan.cpp", "api.hip", "assemble.hip", "attn_f32.hip", "attn_bf16.hip", "decode.hip", "select.hip", "store.cpp",
-           "position.hip", "q4.hip", "q4_attn.hip", "q4_attn_many.hip"]
+           "position.hip", "q4.hip", "q4_attn.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          # packed fp32 instructions are switched off for device code
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -17,15 +17,26 @@
 // by columns of four tokens, nothing goes through LDS either.  Softmax statistics are per lane; the reference point m of a
 // column moves only when a score exceeds it by 2^8, the one case where lanes exchange it.
 //
-// A workgroup of four wavefronts takes a split of a request's keys for one kv head and 16 rows; its wavefronts take the
+// With more than eight rows vector instructions are what it costs, so there the lows go through the matrix cores as well: the
+// pairs of K as they lie in the cache, (scale, low), against (-sum(q), sum(q) / 16) in three bf16 parts; those of V, taken apart
+// into rows of scales and of lows, against the weights in two.  A V that is no number would reach rows that do not see it
+// that way (0 * inf), so units that not every row sees whole keep to the vector instructions.  32 rows a workgroup, two tiles
+// of columns for every operand made of codes: 426 vector instructions for 32 rows, 285 for 16 (81 % of the time they are
+// issued, 32 heads over 8, 4 requests of 8192 tokens with 200 new ones: 216 us, 570 TFLOP/s).
+//
+// A workgroup of four wavefronts takes a split of a request's keys for one kv head and 8 to 32 rows; its wavefronts take the
 // units in turn and meet in LDS at the end.  Where the keys are cut into several splits, a second launch merges them.
-// The kernel is bound by HBM bandwidth as long as enough loads are in flight: every wavefront has two units of LDS of its
-// own, filled by direct global->LDS loads (five a unit, no registers, no barrier) while it works on the other one.
+// With few rows the kernel is bound by HBM bandwidth as long as enough loads are in flight: every wavefront has two units of LDS
+// of its own (three with 32 rows, where fewer wavefronts are there), filled by direct global->LDS loads (five a unit, no
+// registers, no barrier) while it works on another one.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
 
-#include "q4_attn.h"
+#include "common.h"
+#include "mpic_q4.h"
+#include "q4.h"
+#include "wave_ops.h"
 
 namespace mpic {
 namespace {
@@ -33,6 +44,81 @@ namespace {
 using namespace q4;
 
 constexpr int kWaves = 4;
+constexpr int kUnit = 32;            // tokens a wavefront takes at a time: two blocks
+constexpr float kSlack = 8.0f;       // a column's reference point may lag behind its greatest score by this much, log2 units
+constexpr float kLowest = -3e38f;    // reference point of a column that has seen nothing
+constexpr float kLn2 = 0.6931471805599453f;
+
+// s_waitcnt lgkmcnt(0) only
+#define MPIC_WAIT_LGKMCNT0() __builtin_amdgcn_s_waitcnt(0xC07F)
+
+struct Q4AttnArgs {
+  const char* q;
+  const char* cache;
+  const int32_t* q_off;
+  const int32_t* table;
+  const int32_t* lens;
+  char* out;
+  float* lse;
+  float* ws_o;    // [rows][Hq][n_splits][D] normalised partial outputs
+  float* ws_lse;  // [rows][Hq][n_splits] their log-sum-exp in log2 units, -inf: nothing seen
+  int64_t n_rows, q_stride, table_width;  // q_stride in bytes
+  int32_t n_blocks, page_blocks, max_q, max_len, n_splits, n_q_heads, n_kv_heads, group;
+  int32_t split_units;  // units of a split
+  float scale_log2;  // softmax_scale * log2(e)
+};
+
+// Queries of a request, within what the arguments allow whatever the device arrays hold
+struct Request {
+  int64_t first;  // first row
+  int n, len;
+};
+__device__ inline Request request_of(const Q4AttnArgs& a, int b) {
+  Request r;
+  r.len = min(max(a.lens[b], 0), a.max_len);
+  if (!a.q_off) {
+    r.first = b;
+    r.n = 1;
+  } else {
+    const int64_t lo = min(max(static_cast<int64_t>(a.q_off[b]), int64_t{0}), a.n_rows);
+    const int64_t hi = min(max(static_cast<int64_t>(a.q_off[b + 1]), lo), a.n_rows);
+    r.first = lo;
+    r.n = static_cast<int>(min(hi - lo, static_cast<int64_t>(a.max_q)));
+    // (the queries belong to the last tokens: those beyond max_q are the last of them)
+    r.len = static_cast<int>(max(static_cast<int64_t>(r.len) - (hi - lo - r.n), int64_t{0}));
+  }
+  return r;
+}
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+// Two codes of a word as two bf16: those in bits 4n.. and 16 + 4n.., as 1 + code / 16, or exactly (for fp32) as code - 8
+template <bool kExact, int n>
+__device__ inline uint32_t pair_of(uint32_t w) {
+  if (kExact) {
+    const float lo = static_cast<float>(w >> (4 * n) & 15u) - 8.f, hi = static_cast<float>(w >> (16 + 4 * n) & 15u) - 8.f;
+    return __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, hi), __builtin_bit_cast(uint32_t, lo), 0x07060302u);
+  }
+  const uint32_t moved = n == 0 ? w << 3 : w >> (4 * n - 3);
+  // (one instruction, which takes a single constant from a scalar register: the mask stands in a vector register)
+  uint32_t r;
+  asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(r) : "v"(moved), "v"(0x00780078u), "s"(0x3F803F80u));
+  return r;
+}
+template <bool kExact>
+__device__ inline bf16x8 keys_of(uint32_t w) {
+  const u32x4 r = {pair_of<kExact, 0>(w), pair_of<kExact, 1>(w), pair_of<kExact, 2>(w), pair_of<kExact, 3>(w)};
+  return __builtin_bit_cast(bf16x8, r);
+}
+// columns 2 * half and 2 * half + 1 of a V word of both blocks: tokens (0, 2), (1, 3) of either
+template <bool kExact, int odd>
+__device__ inline bf16x8 values_of(uint32_t w0, uint32_t w1) {
+  const u32x4 r = {pair_of<kExact, odd>(w0), pair_of<kExact, 2 + odd>(w0), pair_of<kExact, odd>(w1), pair_of<kExact, 2 + odd>(w1)};
+  return __builtin_bit_cast(bf16x8, r);
+}
+
+__device__ inline f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
 template <int kParts>
 struct Parts {
@@ -53,8 +139,10 @@ __device__ inline Parts<kParts> split_parts(f32x8 x) {
 // How a wavefront's tiles of 16 columns are used.  Wide: a column is a row, and a lane works on all groups of its tokens.
 // Narrow (head_dim 128, up to eight rows): the eight rows stand in the columns twice, the lower eight columns work on the
 // first group of 64 values, the upper eight on the second.  A lane then reads, unpacks and applies the pairs of one group
-// only, and what it lacks of a score is in the lane eight further: 270 instead of 400 vector instructions a unit.
-template <typename T, int D, bool kNarrow_>
+// only, and what it lacks of a score is in the lane eight further: four wavefronts fit a SIMD instead of three (24 contexts of
+// up to 32K tokens 87 us against 92 with a wide tile, 4 of 19841 17.4 against 18.6).
+// Folded: lows through the matrix cores (fp32 pairs would not fit its operands, narrow tiles would gain nothing).
+template <typename T, int D, bool kNarrow_, int kTiles_ = 1>
 struct Shape {
   using Type = T;
   using B = Block<T, D>;
@@ -64,10 +152,15 @@ struct Shape {
   static constexpr int kParts = kExact ? 3 : 1;
   static constexpr int kGroups = B::kGroups;
   static constexpr int kLaneGroups = kNarrow ? 1 : kGroups;  // groups a lane works on
-  static constexpr int kRows = kNarrow ? 8 : 16;  // flattened rows of a workgroup
+  static constexpr bool kFolded = !kExact && !kNarrow;
+  static constexpr int kTiles = kTiles_;                // of columns
+  static constexpr int kRing = kTiles > 1 ? 3 : 2;      // units of LDS of a wavefront
+  static constexpr int kTileRows = kNarrow ? 8 : 16;
+  static constexpr int kRows = kTiles * kTileRows;      // flattened rows of a workgroup
   static constexpr int kWords = B::kLaneBytes / 4;
   static constexpr float kCode = kExact ? 1.f : 16.f;  // what a product with the codes has to be multiplied with
   static_assert(!kNarrow || (kGroups == 2 && !kExact), "two groups share the columns");
+  static_assert(!kFolded || kGroups == 2, "four sums of two groups");
 };
 
 // A unit in LDS: the codes of its two blocks (K, then V), then the pairs of the first block (K, V), then of the second
@@ -131,9 +224,11 @@ template <typename S>
 struct Columns {
   Parts<S::kParts> q[S::kGroups][2];  // (narrow: zeros where a column does not work on the group)
   float q_sum[S::kLaneGroups];
+  bf16x8 q_pairs;              // folded: what the pairs of K meet, (-sum(q), sum(q) / 16) of both groups in parts
   f32x4 o[S::kGroups][4];      // O^T: lane (column, quarter c) holds columns 64 g + 16 c + 4 r + tile of the output
   f32x4 ones[S::kLaneGroups];  // sums of the rounded weights
-  float low[S::kLaneGroups];   // sum p * (low + 8 scale), this lane's tokens
+  f32x4 sums;                  // folded: sums p scale of both groups, then p low
+  float low[S::kLaneGroups];   // sum p * (low + 8 scale), this lane's tokens (folded: of masked units)
   float m, l;                  // reference point (log2 units, the same in the lanes of a column), sum p of this lane's tokens
   int limit;                   // positions 0 .. limit - 1 are seen
 };
@@ -146,29 +241,41 @@ __device__ inline float other_half(float x) {
 
 // One unit of 32 tokens.  masked: not every token is seen by every column (or a block is missing: bit of `have`).
 template <typename S>
-__device__ inline void attend_unit(Columns<S>& s, const char* unit, int pos, bool masked, int have, int lane, float factor) {
+__device__ inline void attend_unit(Columns<S> (&s)[S::kTiles], const char* unit, int pos, bool masked, int have, int lane, float factor) {
   using T = typename S::Type;
-  constexpr int D = S::kDim;
+  using U = Unit<T, S::kDim>;
+  constexpr int D = S::kDim, kTiles = S::kTiles;
   typedef typename Held<T, D>::words words;
   typedef typename Held<T, D>::pairs pairs;
   const int quarter = lane >> 4, my_group = S::kNarrow ? (lane >> 3 & 1) : 0;
-  float x[2][4];
+  float x[kTiles][2][4];
 #pragma unroll
   for (int b = 0; b < 2; ++b) {
     const words k = codes_in<T, D, false>(unit, b, lane);
-    f32x4 acc[S::kLaneGroups];
+    f32x4 acc[kTiles][S::kLaneGroups], lows[kTiles];
+    if (S::kFolded) {
+      const uint32_t pair = *reinterpret_cast<const uint32_t*>(unit + 2 * U::kCodes + b * U::kPairs + ((quarter & 1) * kTokens + (lane & 15)) * 4);
+      const u32x4 four = {pair, pair, pair, pair};
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t) lows[t] = mfma(__builtin_bit_cast(bf16x8, four), s[t].q_pairs, f32x4{0});
+    }
 #pragma unroll
     for (int g = 0; g < S::kGroups; ++g) {
       const int lg = S::kNarrow ? 0 : g;
-      if (!S::kNarrow || g == 0) acc[lg] = f32x4{0};
       const bf16x8 keys[2] = {keys_of<S::kExact>(k[2 * g]), keys_of<S::kExact>(k[2 * g + 1])};
-      // (the small parts first)
 #pragma unroll
-      for (int i = S::kParts - 1; i >= 0; --i)
+      for (int t = 0; t < kTiles; ++t) {
+        if (!S::kNarrow || g == 0) acc[t][lg] = f32x4{0};
+        // (the small parts first)
 #pragma unroll
-        for (int w = 0; w < 2; ++w) acc[lg] = mfma(keys[w], s.q[g][w].p[i], acc[lg]);
+        for (int i = S::kParts - 1; i >= 0; --i)
+#pragma unroll
+          for (int w = 0; w < 2; ++w) acc[t][lg] = mfma(keys[w], s[t].q[g][w].p[i], acc[t][lg]);
+      }
     }
-    f32x4 sum = f32x4{0};
+    f32x4 sum[kTiles];
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) sum[t] = S::kFolded ? lows[t] : f32x4{0};
 #pragma unroll
     for (int g = 0; g < S::kLaneGroups; ++g) {
       const pairs p = pairs_in<T, D, false>(unit, b, S::kNarrow ? my_group : g, quarter);
@@ -177,84 +284,142 @@ __device__ inline void attend_unit(Columns<S>& s, const char* unit, int pos, boo
         const float scale = static_cast<float>(p[2 * r]);
         float low = static_cast<float>(p[2 * r + 1]);
         low = fmaf(S::kExact ? 8.f : -16.f, scale, low);  // (what the codes' operands lack, or have too much)
-        sum[r] = fmaf(scale, acc[g][r], g ? fmaf(low, s.q_sum[g], sum[r]) : low * s.q_sum[g]);
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t)
+          sum[t][r] = fmaf(scale, acc[t][g][r], S::kFolded ? sum[t][r] : g ? fmaf(low, s[t].q_sum[g], sum[t][r]) : low * s[t].q_sum[g]);
       }
     }
 #pragma unroll
-    for (int r = 0; r < 4; ++r) x[b][r] = S::kNarrow ? sum[r] + other_half(sum[r]) : sum[r];
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) x[t][b][r] = S::kNarrow ? sum[t][r] + other_half(sum[t][r]) : sum[t][r];
   }
-  if (masked)
+  if (masked) {
+    asm volatile("");  // (a branch: few units are, and the others should not pay for it)
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const bool seen = (have >> b & 1) && pos + kTokens * b + 4 * quarter + r < s.limit;
-        x[b][r] = seen ? x[b][r] : -INFINITY;
-      }
-  float top = x[0][0];
-#pragma unroll
-  for (int i = 1; i < 8; ++i) top = fmaxf(top, x[i / 4][i % 4]);
-  top *= factor;
-  if (__any(top > s.m + kSlack)) {
-    float m = fmaxf(s.m, top);
-    m = fmaxf(m, __shfl_xor(m, 16));
-    m = fmaxf(m, __shfl_xor(m, 32));
-    const float f = __builtin_amdgcn_exp2f(s.m - m);
-    s.m = m;
-    s.l *= f;
-#pragma unroll
-    for (int g = 0; g < S::kLaneGroups; ++g) {
-      s.low[g] *= f;
-      if (!S::kExact) s.ones[g] *= f;
-    }
-#pragma unroll
-    for (int g = 0; g < S::kGroups; ++g)
-#pragma unroll
-      for (int c = 0; c < 4; ++c) s.o[g][c] *= f;
-  }
-  float p[2][4], scaled[S::kLaneGroups][2][4], low[S::kLaneGroups][2][4];
-#pragma unroll
-  for (int b = 0; b < 2; ++b) {
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      p[b][r] = __builtin_amdgcn_exp2f(fmaf(x[b][r], factor, -s.m));
-      s.l += p[b][r];
-    }
-#pragma unroll
-    for (int g = 0; g < S::kLaneGroups; ++g) {
-      const pairs vp = pairs_in<T, D, true>(unit, b, S::kNarrow ? my_group : g, quarter);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        scaled[g][b][r] = p[b][r] * static_cast<float>(vp[2 * r]);
-        low[g][b][r] = fmaf(8.f, scaled[g][b][r], p[b][r] * static_cast<float>(vp[2 * r + 1]));
-      }
-    }
-  }
-  if (masked)  // (the pairs of what is not seen may be no number)
-#pragma unroll
-    for (int g = 0; g < S::kLaneGroups; ++g)
+    for (int t = 0; t < kTiles; ++t)
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (x[b][r] == -INFINITY) scaled[g][b][r] = low[g][b][r] = 0.f;
-  Parts<S::kParts> weights[S::kLaneGroups];
+        for (int r = 0; r < 4; ++r) {
+          const bool seen = (have >> b & 1) && pos + kTokens * b + 4 * quarter + r < s[t].limit;
+          x[t][b][r] = seen ? x[t][b][r] : -INFINITY;
+        }
+  }
+  float p[kTiles][2][4];
 #pragma unroll
-  for (int g = 0; g < S::kLaneGroups; ++g) {
-    f32x8 w;
+  for (int t = 0; t < kTiles; ++t) {
+    float top = x[t][0][0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) top = fmaxf(top, x[t][i / 4][i % 4]);
+    top *= factor;
+    if (__any(top > s[t].m + kSlack)) {
+      float m = fmaxf(s[t].m, top);
+      m = fmaxf(m, __shfl_xor(m, 16));
+      m = fmaxf(m, __shfl_xor(m, 32));
+      const float f = __builtin_amdgcn_exp2f(s[t].m - m);
+      s[t].m = m;
+      s[t].l *= f;
+      if (S::kFolded) s[t].sums *= f;
+#pragma unroll
+      for (int g = 0; g < S::kLaneGroups; ++g) {
+        s[t].low[g] *= f;
+        if (!S::kExact) s[t].ones[g] *= f;
+      }
+#pragma unroll
+      for (int g = 0; g < S::kGroups; ++g)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) s[t].o[g][c] *= f;
+    }
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        w[4 * b + (r & 1) * 2 + (r >> 1)] = scaled[g][b][r];  // tokens (0, 2), (1, 3)
-        s.low[g] += low[g][b][r];
+        p[t][b][r] = __builtin_amdgcn_exp2f(fmaf(x[t][b][r], factor, -s[t].m));
+        s[t].l += p[t][b][r];
       }
-    weights[g] = split_parts<S::kParts>(w);
   }
+  float scaled[kTiles][S::kLaneGroups][2][4], low[kTiles][S::kLaneGroups][2][4];
+#pragma unroll
+  for (int g = 0; g < S::kLaneGroups; ++g)
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const pairs vp = pairs_in<T, D, true>(unit, b, S::kNarrow ? my_group : g, quarter);
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          scaled[t][g][b][r] = p[t][b][r] * static_cast<float>(vp[2 * r]);
+          if (!S::kFolded) low[t][g][b][r] = fmaf(8.f, scaled[t][g][b][r], p[t][b][r] * static_cast<float>(vp[2 * r + 1]));
+        }
+    }
+  if (masked) {  // (the pairs of what is not seen may be no number)
+    asm volatile("");
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+      for (int g = 0; g < S::kLaneGroups; ++g)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          pairs vp;
+          if (S::kFolded) vp = pairs_in<T, D, true>(unit, b, g, quarter);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            if (S::kFolded) low[t][g][b][r] = fmaf(8.f, scaled[t][g][b][r], p[t][b][r] * static_cast<float>(vp[2 * r + 1]));
+            if (x[t][b][r] == -INFINITY) scaled[t][g][b][r] = low[t][g][b][r] = 0.f;
+            if (S::kFolded) s[t].low[g] += low[t][g][b][r];
+          }
+        }
+  } else if (S::kFolded) {
+    // rows of the operand, four times over: the scales of both groups, then the lows; tokens as in the weights
+    const char* at = unit + 2 * U::kCodes + U::B::kPairs + ((lane & 1) * kTokens + 4 * quarter) * 4;
+    const uint32_t take = lane & 2 ? 0x07060302u : 0x05040100u;
+    u32x4 four;
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const u32x4 raw = *reinterpret_cast<const u32x4*>(at + b * U::kPairs);
+      four[2 * b] = __builtin_amdgcn_perm(raw[2], raw[0], take);
+      four[2 * b + 1] = __builtin_amdgcn_perm(raw[3], raw[1], take);
+    }
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+      // the weights in two parts: their upper halves as they are, and what is left
+      u32x4 high;
+      f32x8 rest;
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const uint32_t x0 = __builtin_bit_cast(uint32_t, p[t][b][r]), x2 = __builtin_bit_cast(uint32_t, p[t][b][r + 2]);
+          high[2 * b + r] = __builtin_amdgcn_perm(x2, x0, 0x07060302u);
+          rest[4 * b + 2 * r] = p[t][b][r] - __builtin_bit_cast(float, x0 & 0xFFFF0000u);
+          rest[4 * b + 2 * r + 1] = p[t][b][r + 2] - __builtin_bit_cast(float, x2 & 0xFFFF0000u);
+        }
+      s[t].sums = mfma(__builtin_bit_cast(bf16x8, four), __builtin_convertvector(rest, bf16x8), s[t].sums);
+      s[t].sums = mfma(__builtin_bit_cast(bf16x8, four), __builtin_bit_cast(bf16x8, high), s[t].sums);
+    }
+  }
+  Parts<S::kParts> weights[kTiles][S::kLaneGroups];
+#pragma unroll
+  for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+    for (int g = 0; g < S::kLaneGroups; ++g) {
+      f32x8 w;
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          w[4 * b + (r & 1) * 2 + (r >> 1)] = scaled[t][g][b][r];  // tokens (0, 2), (1, 3)
+          if (!S::kFolded) s[t].low[g] += low[t][g][b][r];
+        }
+      weights[t][g] = split_parts<S::kParts>(w);
+    }
   if (!S::kExact) {
     const u32x4 one = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
 #pragma unroll
-    for (int g = 0; g < S::kLaneGroups; ++g) s.ones[g] = mfma(__builtin_bit_cast(bf16x8, one), weights[g].p[0], s.ones[g]);
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+      for (int g = 0; g < S::kLaneGroups; ++g) s[t].ones[g] = mfma(__builtin_bit_cast(bf16x8, one), weights[t][g].p[0], s[t].ones[g]);
   }
   const words v0 = codes_in<T, D, true>(unit, 0, lane), v1 = codes_in<T, D, true>(unit, 1, lane);
 #pragma unroll
@@ -263,10 +428,12 @@ __device__ inline void attend_unit(Columns<S>& s, const char* unit, int pos, boo
     for (int c = 0; c < 2; ++c) {
       const bf16x8 even = values_of<S::kExact, 0>(v0[2 * g + c], v1[2 * g + c]), odd = values_of<S::kExact, 1>(v0[2 * g + c], v1[2 * g + c]);
 #pragma unroll
-      for (int i = S::kParts - 1; i >= 0; --i) {
-        s.o[g][2 * c] = mfma(even, weights[S::kNarrow ? 0 : g].p[i], s.o[g][2 * c]);
-        s.o[g][2 * c + 1] = mfma(odd, weights[S::kNarrow ? 0 : g].p[i], s.o[g][2 * c + 1]);
-      }
+      for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+        for (int i = S::kParts - 1; i >= 0; --i) {
+          s[t].o[g][2 * c] = mfma(even, weights[t][S::kNarrow ? 0 : g].p[i], s[t].o[g][2 * c]);
+          s[t].o[g][2 * c + 1] = mfma(odd, weights[t][S::kNarrow ? 0 : g].p[i], s[t].o[g][2 * c + 1]);
+        }
     }
 }
 
@@ -275,8 +442,8 @@ template <typename S>
 struct AttnLds {
   using U = Unit<typename S::Type, S::kDim>;
   static constexpr int kRow = S::kDim + 4;
-  static constexpr int kWave = 2 * U::kBytes;
-  static constexpr int kMerge = kWaves * S::kRows * (kRow + 2) * 4;
+  static constexpr int kWave = S::kRing * U::kBytes;
+  static constexpr int kMerge = kWaves * S::kTileRows * (kRow + 2) * 4;
   static constexpr int kBytes = kWaves * kWave > kMerge ? kWaves * kWave : kMerge;
   static_assert(kBytes <= 65536, "no opt-in needed");
 };
@@ -289,12 +456,12 @@ __global__ __launch_bounds__(kWaves * 64, kWavesPerSimd) void q4_attn_kernel(Q4A
   using L = AttnLds<S>;
   using U = Unit<T, D>;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
-  typedef float PartRows[S::kRows][L::kRow];
-  typedef float PartCols[S::kRows];
+  typedef float PartRows[S::kTileRows][L::kRow];
+  typedef float PartCols[S::kTileRows];
   PartRows* part_o = reinterpret_cast<PartRows*>(lds);
   PartCols* part_m = reinterpret_cast<PartCols*>(part_o + kWaves);
   PartCols* part_l = part_m + kWaves;
-  const int lane = threadIdx.x & 63, col = lane & (S::kRows - 1), quarter = lane >> 4;
+  const int lane = threadIdx.x & 63, col = lane & (S::kTileRows - 1), quarter = lane >> 4;
   const int my_group = S::kNarrow ? (lane >> 3 & 1) : 0;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // heads first: neighbouring workgroups go to different L2 domains, which thus get the same share of every split, and the
@@ -322,17 +489,18 @@ __global__ __launch_bounds__(kWaves * 64, kWavesPerSimd) void q4_attn_kernel(Q4A
   const int unit_end = min((key_end + kUnit - 1) / kUnit, (split + 1) * a.split_units);
   if (a.n_splits > 1 && unit_end <= split * a.split_units) return;  // (the merge asks for no such split)
 
-  Columns<S> s;
+  Columns<S> s[S::kTiles];
   typedef T vec __attribute__((ext_vector_type(8), aligned(16)));
-  vec raw[S::kGroups][2];
-  {
-    const int at = row0 + col, flat = min(at, n_flat - 1), token = flat / a.group, hq = head * a.group + flat % a.group;
-    s.limit = at < n_flat ? behind + token + 1 : 0;
+  vec raw[S::kTiles][S::kGroups][2];
+#pragma unroll
+  for (int t = 0; t < S::kTiles; ++t) {
+    const int at = row0 + t * S::kTileRows + col, flat = min(at, n_flat - 1), token = flat / a.group, hq = head * a.group + flat % a.group;
+    s[t].limit = at < n_flat ? behind + token + 1 : 0;
     const char* q = a.q + (rq.first + token) * a.q_stride + static_cast<int64_t>(hq) * D * sizeof(T);
 #pragma unroll
     for (int g = 0; g < S::kGroups; ++g)
 #pragma unroll
-      for (int w = 0; w < 2; ++w) raw[g][w] = *reinterpret_cast<const vec*>(q + (g * kGroup + quarter * 16 + w * 8) * sizeof(T));
+      for (int w = 0; w < 2; ++w) raw[t][g][w] = *reinterpret_cast<const vec*>(q + (g * kGroup + quarter * 16 + w * 8) * sizeof(T));
   }
   const int n_units = unit_end > unit0 ? (unit_end - unit0 + kWaves - 1) / kWaves : 0;  // of this wavefront
   // the blocks of the next 32 units, two lanes a unit; -1: not in the cache
@@ -346,111 +514,141 @@ __global__ __launch_bounds__(kWaves * 64, kWavesPerSimd) void q4_attn_kernel(Q4A
   char* ring = lds + wave * L::kWave;
   const uint32_t ring_lds = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(MPIC_LDS_PTR(char, ring)));
   // load unit i of this wavefront into its half of the ring; bit b of the result: block b is in the cache
+  int ring_at = 0;  // of unit i to be staged
   auto stage = [&](int i) {
     if ((i & 31) == 0) look_up(i);
     const int id0 = __builtin_amdgcn_readlane(ids, 2 * i & 63), id1 = __builtin_amdgcn_readlane(ids, (2 * i & 63) + 1);
     const char* base = a.cache + static_cast<int64_t>(head) * B::kBytes;
     const int64_t pitch = static_cast<int64_t>(a.n_kv_heads) * B::kBytes;
-    stage_unit<T, D>(base + max(id0, 0) * pitch, base + max(id1, 0) * pitch, lane, ring_lds + (i & 1) * U::kBytes);
+    stage_unit<T, D>(base + max(id0, 0) * pitch, base + max(id1, 0) * pitch, lane, ring_lds + ring_at);
+    ring_at = ring_at == (S::kRing - 1) * U::kBytes ? 0 : ring_at + U::kBytes;
     return (id0 >= 0 ? 1 : 0) | (id1 >= 0 ? 2 : 0);
   };
-  int have = 0;
+  int have = 0, have_next = 0;
   if (n_units > 0) have = stage(0);
-  s.m = kLowest;
-  s.l = 0.f;
+  if (S::kRing > 2 && n_units > 1) have_next = stage(1);
 #pragma unroll
-  for (int g = 0; g < S::kLaneGroups; ++g) s.q_sum[g] = s.low[g] = 0.f, s.ones[g] = f32x4{0};
+  for (int t = 0; t < S::kTiles; ++t) {
+    s[t].m = kLowest;
+    s[t].l = 0.f;
+    s[t].sums = f32x4{0};
 #pragma unroll
-  for (int g = 0; g < S::kGroups; ++g) {
-    const int lg = S::kNarrow ? 0 : g;
+    for (int g = 0; g < S::kLaneGroups; ++g) s[t].q_sum[g] = s[t].low[g] = 0.f, s[t].ones[g] = f32x4{0};
 #pragma unroll
-    for (int c = 0; c < 4; ++c) s.o[g][c] = f32x4{0};
+    for (int g = 0; g < S::kGroups; ++g) {
+      const int lg = S::kNarrow ? 0 : g;
 #pragma unroll
-    for (int w = 0; w < 2; ++w) {
-      f32x8 x = __builtin_convertvector(raw[g][w], f32x8);
-      if (S::kNarrow && g != my_group) x = f32x8{0};
-      s.q[g][w] = split_parts<S::kParts>(x);
+      for (int c = 0; c < 4; ++c) s[t].o[g][c] = f32x4{0};
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s.q_sum[lg] += x[e];
+      for (int w = 0; w < 2; ++w) {
+        f32x8 x = __builtin_convertvector(raw[t][g][w], f32x8);
+        if (S::kNarrow && g != my_group) x = f32x8{0};
+        s[t].q[g][w] = split_parts<S::kParts>(x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[t].q_sum[lg] += x[e];
+      }
+    }
+#pragma unroll
+    for (int g = 0; g < S::kLaneGroups; ++g) {
+      s[t].q_sum[g] += __shfl_xor(s[t].q_sum[g], 16);
+      s[t].q_sum[g] += __shfl_xor(s[t].q_sum[g], 32);
+      s[t].q_sum[g] *= 1.f / S::kCode;
+    }
+    if (S::kFolded) {
+      // a product of (scale, low) pairs with (-sum(q), sum(q) / 16): of one group per quarter, its three bf16 parts one after
+      // the other; two quarters have nothing
+      const float sum = quarter == 0 ? s[t].q_sum[0] : quarter == 1 ? s[t].q_sum[S::kLaneGroups - 1] : 0.f;
+      f32x8 x = f32x8{0};
+      float rest = sum;
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {
+        const float part = static_cast<float>(static_cast<__bf16>(rest));
+        x[2 * i] = -16.f * part;
+        x[2 * i + 1] = part;
+        rest -= part;
+      }
+      s[t].q_pairs = __builtin_convertvector(x, bf16x8);
     }
   }
-#pragma unroll
-  for (int g = 0; g < S::kLaneGroups; ++g) {
-    s.q_sum[g] += __shfl_xor(s.q_sum[g], 16);
-    s.q_sum[g] += __shfl_xor(s.q_sum[g], 32);
-    s.q_sum[g] *= 1.f / S::kCode;
-  }
   const float factor = a.scale_log2 * S::kCode;
+  int unit_at = 0;
   for (int i = 0; i < n_units; ++i) {
-    int have_next = 0;
-    // what was read of the half that is loaded next has arrived (all of it has been used, but nothing else orders the two)
+    // what was read of the unit that is loaded next has arrived (all of it has been used, but nothing else orders the two)
     MPIC_WAIT_LGKMCNT0();
     asm volatile("" ::: "memory");
-    if (i + 1 < n_units) {
-      have_next = stage(i + 1);
+    int have_last = 0;
+    if (i + S::kRing - 1 < n_units) {
+      have_last = stage(i + S::kRing - 1);
+      MPIC_WAIT_VMCNT((S::kRing - 1) * U::kLoads);
+    } else if (S::kRing > 2 && i + 1 < n_units) {
       MPIC_WAIT_VMCNT(U::kLoads);
     } else {
       MPIC_WAIT_VMCNT(0);
     }
     asm volatile("" ::: "memory");
-    const char* unit = ring + (i & 1) * U::kBytes;
     const int pos = (unit0 + i * kWaves) * kUnit;
-    attend_unit(s, unit, pos, have != 3 || pos + kUnit > key_all, have, lane, factor);
-    have = have_next;
+    attend_unit(s, ring + unit_at, pos, have != 3 || pos + kUnit > key_all, have, lane, factor);
+    unit_at = unit_at == (S::kRing - 1) * U::kBytes ? 0 : unit_at + U::kBytes;
+    have = S::kRing > 2 ? have_next : have_last;
+    have_next = have_last;
   }
 
-  __syncthreads();  // (the ring has been read)
-  s.l += __shfl_xor(s.l, 16);
-  s.l += __shfl_xor(s.l, 32);
-  if (lane < S::kRows) {
-    part_m[wave][col] = s.m;
-    part_l[wave][col] = s.l;
-  }
 #pragma unroll
-  for (int g = 0; g < S::kLaneGroups; ++g) {
-    s.low[g] += __shfl_xor(s.low[g], 16);
-    s.low[g] += __shfl_xor(s.low[g], 32);
-    const int group = S::kNarrow ? my_group : g;
+  for (int t = 0; t < S::kTiles; ++t) {
+    __syncthreads();  // (the ring has been read, or the tile in front)
+    s[t].l += __shfl_xor(s[t].l, 16);
+    s[t].l += __shfl_xor(s[t].l, 32);
+    if (lane < S::kTileRows) {
+      part_m[wave][col] = s[t].m;
+      part_l[wave][col] = s[t].l;
+    }
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      f32x4 o;
+    for (int g = 0; g < S::kLaneGroups; ++g) {
+      s[t].low[g] += __shfl_xor(s[t].low[g], 16);
+      s[t].low[g] += __shfl_xor(s[t].low[g], 32);
+      if (S::kFolded) s[t].low[g] += fmaf(8.f, s[t].sums[g & 1], s[t].sums[2 + (g & 1)]);
+      const int group = S::kNarrow ? my_group : g;
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const float sum = S::kNarrow && my_group ? s.o[S::kGroups - 1][c][r] : s.o[g][c][r];
-        o[c] = S::kExact ? sum + s.low[g] : fmaf(fmaf(-1.5f, s.ones[g][r], sum), S::kCode, s.low[g]);
+      for (int r = 0; r < 4; ++r) {
+        f32x4 o;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const float sum = S::kNarrow && my_group ? s[t].o[S::kGroups - 1][c][r] : s[t].o[g][c][r];
+          o[c] = S::kExact ? sum + s[t].low[g] : fmaf(fmaf(-1.5f, s[t].ones[g][r], sum), S::kCode, s[t].low[g]);
+        }
+        *reinterpret_cast<f32x4*>(&part_o[wave][col][group * kGroup + quarter * 16 + 4 * r]) = o;
       }
-      *reinterpret_cast<f32x4*>(&part_o[wave][col][group * kGroup + quarter * 16 + 4 * r]) = o;
     }
-  }
-  __syncthreads();
+    __syncthreads();
 
-  constexpr int kThreads = kWaves * 64 / S::kRows, kEach = D / kThreads;  // threads and values per row
-  typedef float each __attribute__((ext_vector_type(kEach), aligned(16)));
-  const int c = threadIdx.x / kThreads, d0 = threadIdx.x % kThreads * kEach, at = row0 + c;
-  if (at < n_flat) {
-    float top = part_m[0][c];
+    constexpr int kThreads = kWaves * 64 / S::kTileRows, kEach = D / kThreads;  // threads and values per row
+    typedef float each __attribute__((ext_vector_type(kEach), aligned(16)));
+    const int c = threadIdx.x / kThreads, d0 = threadIdx.x % kThreads * kEach, at = row0 + t * S::kTileRows + c;
+    if (at < n_flat) {
+      float top = part_m[0][c];
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) top = fmaxf(top, part_m[w][c]);
-    float z = 0.f;
-    each o = each{0};
+      for (int w = 1; w < kWaves; ++w) top = fmaxf(top, part_m[w][c]);
+      float z = 0.f;
+      each o = each{0};
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      const float f = __builtin_amdgcn_exp2f(part_m[w][c] - top);
-      z = fmaf(f, part_l[w][c], z);
-      o += *reinterpret_cast<const each*>(&part_o[w][c][d0]) * f;
-    }
-    const bool none = z == 0.f;
-    const float inv = none ? 0.f : 1.f / z, lse2 = none ? -INFINITY : top + log2f(z);
-    o *= inv;
-    const int64_t row = (rq.first + at / a.group) * a.n_q_heads + head * a.group + at % a.group;
-    if (a.n_splits > 1) {
-      const int64_t part = row * a.n_splits + split;
-      if (d0 == 0) a.ws_lse[part] = lse2;
-      if (!none) *reinterpret_cast<each*>(a.ws_o + part * D + d0) = o;
-    } else {
-      typedef T vec __attribute__((ext_vector_type(kEach), aligned(8)));
-      *reinterpret_cast<vec*>(a.out + (row * D + d0) * sizeof(T)) = __builtin_convertvector(o, vec);
-      if (a.lse && d0 == 0) a.lse[row] = lse2 * kLn2;
+      for (int w = 0; w < kWaves; ++w) {
+        const float f = __builtin_amdgcn_exp2f(part_m[w][c] - top);
+        z = fmaf(f, part_l[w][c], z);
+        o += *reinterpret_cast<const each*>(&part_o[w][c][d0]) * f;
+      }
+      const bool none = z == 0.f;
+      const float inv = none ? 0.f : 1.f / z, lse2 = none ? -INFINITY : top + log2f(z);
+      o *= inv;
+      const int64_t row = (rq.first + at / a.group) * a.n_q_heads + head * a.group + at % a.group;
+      if (a.n_splits > 1) {
+        const int64_t part = row * a.n_splits + split;
+        if (d0 == 0) a.ws_lse[part] = lse2;
+        if (!none) *reinterpret_cast<each*>(a.ws_o + part * D + d0) = o;
+      } else {
+        typedef T vec __attribute__((ext_vector_type(kEach), aligned(8)));
+        *reinterpret_cast<vec*>(a.out + (row * D + d0) * sizeof(T)) = __builtin_convertvector(o, vec);
+        if (a.lse && d0 == 0) a.lse[row] = lse2 * kLn2;
+      }
     }
   }
 }
@@ -470,7 +668,7 @@ __global__ __launch_bounds__(256) void q4_merge_kernel(Q4AttnArgs a) {
   const float* part = a.ws_lse + row * a.n_splits;
   // splits that hold keys of this row
   const int keys = i < n_rows ? max(rq.len - rq.n + static_cast<int>(i / a.n_q_heads) + 1, 0) : 0;
-  const int n_splits = keys > 0 ? min(((keys - 1) / kUnit) / units_of_split(a, rq) + 1, a.n_splits) : 0;
+  const int n_splits = keys > 0 ? min(((keys - 1) / kUnit) / a.split_units + 1, a.n_splits) : 0;
   // eight splits at a time: their loads do not wait for each other, nor an output for the log-sum-exp that says whether it
   // was written at all
   constexpr int kBatch = 8;
@@ -528,49 +726,50 @@ __global__ __launch_bounds__(256) void q4_merge_kernel(Q4AttnArgs a) {
 
 // Rows of a workgroup and how the keys are cut.
 //
-// The kernel of this file takes 8 or 16 rows a workgroup, the one for many rows 128 of them, which share what is read of the
-// keys: a fifth of the work of a workgroup of 16, but steps that are long and wait for each other.  So it takes over where the
-// launch is large enough that work counts and not the length of a step, by (tiles of 16 rows) * (units of keys) over all kv
-// heads and requests: 23 000 of them 31 us against 27 with 16 rows (28 heads over 4, 2 requests of 7300 tokens, 61 rows each),
-// 51 000 equal, 84 000 64 against 76 (100 rows over 3000 tokens of 32 kv heads), 104 000 76 against 86, and 12 % less in larger
-// ones.  Below 96 rows its tile would be half empty.
+// 8 rows where that is all there is.  Beyond that 16 or 32: a unit of 32 rows costs 1.3 times the instructions of one of 16, but
+// takes longer from its first to its last, and only half as many wavefronts fit.  So 32 rows need a launch that fills the
+// machine, (tiles of 16 rows) * (units of keys) over all kv heads and requests, and no more than a third of its tiles' rows may
+// be without one: 32 heads over 8, 10 400 of those units 20 us either way, 20 600 26 us against 27, 82 000 58 against 74,
+// 410 000 216 against 265; below that 1 to 3 us more (9 rows over 512 tokens 11 us against 8).
 //
 // 8 or 16 rows: splits of whole units for every wavefront, so that three workgroups a compute unit are there where the requests
 // alone do not make them (four would fit with 8 rows, but smaller splits cost more: 4 requests of 19841 tokens 18.5 us
 // against 17.6), and no less than two units a wavefront.  Lengths differ, and a launch is over when its longest split is:
-// splits are cut down to 32 units as long as that makes no more than eight rounds of them.  Five units a wavefront stay in one
-// piece: a further unit takes 0.9 us (4 requests of 128 tokens 4.5 us, of 256 5.4), the merge 2.7 and its launch 2.3 of the host.
-// Many rows: workgroups take longer, so their rounds count (two a compute unit): the number of splits with the least rounds *
-// (units of a split + 5), 5 being what a workgroup and its share of the merge cost besides, no less than 8 units each.
+// splits are cut down to 32 units as long as that makes no more than eight rounds of them.
+// 32 rows: workgroups take longer, so their rounds count (two a compute unit): the number of splits with the least rounds *
+// (units of a split + 16), 16 being what a workgroup and its share of the merge cost besides (2 requests of 16000 tokens with 256
+// new ones 245 us, 272 by the rule above).
+// Five units a wavefront stay in one piece: a further unit takes 0.9 us (4 requests of 128 tokens 4.5 us, of 256 5.4), the
+// merge 2.7 and its launch 2.3 of the host.
 struct Cut {
   int32_t rows;  // flattened rows of a workgroup
-  int32_t n_splits, split_units, split_least;  // (see units_of_split)
+  int32_t n_splits, split_units;
   int64_t tiles;
 };
 Cut cut_of(const mpic_ctx* ctx, int32_t n_requests, int32_t max_q, int64_t max_len) {
-  constexpr int64_t kRound = 768, kRounds = 8, kWhole = 5 * kWaves, kLeast = 2 * kWaves, kMost = 32;
-  constexpr int64_t kFew = 96, kManyWork = 65536, kManyRound = 512, kManyLeast = 8, kManyCost = 5, kManySplits = 64;
+  constexpr int64_t kWhole = 5 * kWaves, kLeast = 2 * kWaves, kRound = 768, kRounds = 8, kMost = 32;
+  constexpr int64_t kRound32 = 512, kCost32 = 16, kSplits32 = 64, kLarge = 16384;
   const int64_t units = std::max<int64_t>(1, (max_len + kUnit - 1) / kUnit), flat = static_cast<int64_t>(max_q) * ctx->group;
+  const int64_t tiles16 = (flat + 15) / 16, tiles32 = (flat + 31) / 32;
+  const double work = static_cast<double>(tiles16 * ctx->cfg.n_kv_heads) * n_requests * units;
   Cut cut{};
-  const double work = static_cast<double>((flat + 15) / 16 * ctx->cfg.n_kv_heads) * n_requests * units;
-  cut.rows = ctx->cfg.dtype != MPIC_BF16 ? 16 : flat <= 8 ? 8 : flat <= kFew || work < kManyWork ? 16 : kManyRows;
+  cut.rows = ctx->cfg.dtype != MPIC_BF16 ? 16 : flat <= 8 ? 8 : work < kLarge || 5 * tiles32 > 3 * tiles16 ? 16 : 32;
   cut.tiles = (flat + cut.rows - 1) / cut.rows;
   const int64_t lanes = cut.tiles * ctx->cfg.n_kv_heads * n_requests;
-  const auto units_of = [&](int64_t splits, int64_t step) { return ((units + splits - 1) / splits + step - 1) / step * step; };
-  int64_t each = 0;
-  if (cut.rows == kManyRows) {
+  const auto units_of = [&](int64_t splits) { return ((units + splits - 1) / splits + kWaves - 1) / kWaves * kWaves; };
+  int64_t each = kWhole;
+  if (units > kWhole && cut.rows == 32) {
     double best = INFINITY;
-    for (int64_t splits = 1; splits <= kManySplits; ++splits) {
-      const int64_t n = std::max(kManyLeast, units_of(splits, kManyUnits)), used = (units + n - 1) / n;
-      const double cost = static_cast<double>((lanes * used + kManyRound - 1) / kManyRound) * (n + kManyCost);
+    for (int64_t splits = 1; splits <= kSplits32; ++splits) {
+      const int64_t n = std::max(kLeast, units_of(splits)), used = (units + n - 1) / n;
+      const double cost = static_cast<double>((lanes * used + kRound32 - 1) / kRound32) * (n + kCost32);
       if (cost >= best) continue;
       best = cost;
       each = n;
     }
-    cut.split_least = lanes * ((units + each - 1) / each) <= kManyRound ? kManyLeast : 0;
-  } else {
-    const auto of_rounds = [&](int64_t rounds) { return units_of(std::max<int64_t>(1, rounds * kRound / lanes), kWaves); };
-    each = units <= kWhole ? kWhole : std::max(kLeast, std::min(of_rounds(1), std::max(kMost, of_rounds(kRounds))));
+  } else if (units > kWhole) {
+    const auto of_rounds = [&](int64_t rounds) { return units_of(std::max<int64_t>(1, rounds * kRound / lanes)); };
+    each = std::max(kLeast, std::min(of_rounds(1), std::max(kMost, of_rounds(kRounds))));
   }
   cut.split_units = static_cast<int32_t>(each);
   cut.n_splits = static_cast<int32_t>((units + each - 1) / each);
@@ -674,8 +873,6 @@ extern "C" int mpic_q4_attn(mpic_ctx* ctx, const void* q, int64_t q_stride, int6
   a.max_len = static_cast<int32_t>(max_len);
   a.n_splits = cut.n_splits;
   a.split_units = cut.split_units;
-  a.split_least = cut.split_least;
-  a.split_step = kManyUnits;
   a.n_q_heads = c.n_q_heads;
   a.n_kv_heads = c.n_kv_heads;
   a.group = ctx->group;
@@ -687,7 +884,7 @@ extern "C" int mpic_q4_attn(mpic_ctx* ctx, const void* q, int64_t q_stride, int6
   else if (c.dtype == MPIC_BF16 && cut.rows == 16)
     MPIC_HIP(ctx, (launch_q4_attn<Shape<__bf16, 128, false>, 3>(a, grid, stream)));
   else if (c.dtype == MPIC_BF16)
-    MPIC_HIP(ctx, launch_q4_attn_many(a, grid, stream));
+    MPIC_HIP(ctx, (launch_q4_attn<Shape<__bf16, 128, false, 2>, 2>(a, grid, stream)));
   else if (c.head_dim == 128)
     MPIC_HIP(ctx, (launch_q4_attn<Shape<float, 128, false>, 3>(a, grid, stream)));
   else
