@@ -22,7 +22,7 @@
 // into rows of scales and of lows, against the weights in two.  A V that is no number would reach rows that do not see it
 // that way (0 * inf), so units that not every row sees whole keep to the vector instructions.  32 rows a workgroup, two tiles
 // of columns for every operand made of codes: 426 vector instructions for 32 rows, 285 for 16 (81 % of the time they are
-// issued, 32 heads over 8, 4 requests of 8192 tokens with 200 new ones: 216 us, 570 TFLOP/s).
+// issued, 32 heads over 8, 4 requests of 8192 tokens with 200 new ones: 221 us, 480 TFLOP/s).
 //
 // A workgroup of four wavefronts takes a split of a request's keys for one kv head and 8 to 32 rows; its wavefronts take the
 // units in turn and meet in LDS at the end.  Where the keys are cut into several splits, a second launch merges them.
@@ -729,8 +729,8 @@ __global__ __launch_bounds__(256) void q4_merge_kernel(Q4AttnArgs a) {
 // 8 rows where that is all there is.  Beyond that 16 or 32: a unit of 32 rows costs 1.3 times the instructions of one of 16, but
 // takes longer from its first to its last, and only half as many wavefronts fit.  So 32 rows need a launch that fills the
 // machine, (tiles of 16 rows) * (units of keys) over all kv heads and requests, and no more than a third of its tiles' rows may
-// be without one: 32 heads over 8, 10 400 of those units 20 us either way, 20 600 26 us against 27, 82 000 58 against 74,
-// 410 000 216 against 265; below that 1 to 3 us more (9 rows over 512 tokens 11 us against 8).
+// be without one: 32 heads over 8, 10 400 of those units 20 us either way, 20 600 25 us against 27, 82 000 57 against 74,
+// 410 000 221 against 265; below that 1 to 3 us more (9 rows over 512 tokens 11 us against 8).
 //
 // 8 or 16 rows: splits of whole units for every wavefront, so that three workgroups a compute unit are there where the requests
 // alone do not make them (four would fit with 8 rows, but smaller splits cost more: 4 requests of 19841 tokens 18.5 us
