@@ -19,7 +19,8 @@
 //
 // With more than eight rows vector instructions are what it costs, so there the lows go through the matrix cores as well: the
 // pairs of K as they lie in the cache, (scale, low), against (-sum(q), sum(q) / 16) in three bf16 parts; those of V, taken apart
-// into rows of scales and of lows, against the weights in two.  A V that is no number would reach rows that do not see it
+// into rows of scales and of lows, against the weights rounded to bf16: that is the middle of a group, low + 8 scale, times a
+// weight off by 2^-8 at most, which is what a context in bf16 costs too.  A V that is no number would reach rows that do not see it
 // that way (0 * inf), so units that not every row sees whole keep to the vector instructions.  32 rows a workgroup, two tiles
 // of columns for every operand made of codes: 426 vector instructions for 32 rows, 285 for 16 (81 % of the time they are
 // issued, 32 heads over 8, 4 requests of 8192 tokens with 200 new ones: 221 us, 480 TFLOP/s).
@@ -239,6 +240,13 @@ __device__ inline float other_half(float x) {
   return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(i, i, 0x128, 0xf, 0xf, true));  // rotation of the row by eight
 }
 
+// (fmaxf makes a second instruction of every operand that may be a signalling NaN; a score that is none shows in its weight)
+__device__ inline float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+
 // One unit of 32 tokens.  masked: not every token is seen by every column (or a block is missing: bit of `have`).
 template <typename S>
 __device__ inline void attend_unit(Columns<S> (&s)[S::kTiles], const char* unit, int pos, bool masked, int have, int lane, float factor) {
@@ -309,10 +317,7 @@ __device__ inline void attend_unit(Columns<S> (&s)[S::kTiles], const char* unit,
   float p[kTiles][2][4];
 #pragma unroll
   for (int t = 0; t < kTiles; ++t) {
-    float top = x[t][0][0];
-#pragma unroll
-    for (int i = 1; i < 8; ++i) top = fmaxf(top, x[t][i / 4][i % 4]);
-    top *= factor;
+    const float top = max3(max3(x[t][0][0], x[t][0][1], x[t][0][2]), max3(x[t][0][3], x[t][1][0], x[t][1][1]), max3(x[t][1][2], x[t][1][3], x[t][1][3])) * factor;
     if (__any(top > s[t].m + kSlack)) {
       float m = fmaxf(s[t].m, top);
       m = fmaxf(m, __shfl_xor(m, 16));
@@ -383,20 +388,12 @@ __device__ inline void attend_unit(Columns<S> (&s)[S::kTiles], const char* unit,
     }
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
-      // the weights in two parts: their upper halves as they are, and what is left
-      u32x4 high;
-      f32x8 rest;
+      f32x8 w;
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          const uint32_t x0 = __builtin_bit_cast(uint32_t, p[t][b][r]), x2 = __builtin_bit_cast(uint32_t, p[t][b][r + 2]);
-          high[2 * b + r] = __builtin_amdgcn_perm(x2, x0, 0x07060302u);
-          rest[4 * b + 2 * r] = p[t][b][r] - __builtin_bit_cast(float, x0 & 0xFFFF0000u);
-          rest[4 * b + 2 * r + 1] = p[t][b][r + 2] - __builtin_bit_cast(float, x2 & 0xFFFF0000u);
-        }
-      s[t].sums = mfma(__builtin_bit_cast(bf16x8, four), __builtin_convertvector(rest, bf16x8), s[t].sums);
-      s[t].sums = mfma(__builtin_bit_cast(bf16x8, four), __builtin_bit_cast(bf16x8, high), s[t].sums);
+        for (int r = 0; r < 4; ++r) w[4 * b + (r & 1) * 2 + (r >> 1)] = p[t][b][r];
+      s[t].sums = mfma(__builtin_bit_cast(bf16x8, four), __builtin_convertvector(w, bf16x8), s[t].sums);
     }
   }
   Parts<S::kParts> weights[kTiles][S::kLaneGroups];

@@ -238,10 +238,10 @@ class Held:
         step = max([float(np.nanmax(h[2])) for h in held[0] if h[2].size] + [0.0])
         score = 2.0 ** -21 * scale * 32 * step * np.abs(q).sum(-1, keepdims=True)
         top = max([float(np.abs(h[0]).max()) for h in held[1] if h[0].size] + [0.0])
-        # Weights times a scale of V are rounded once (bf16 2^-8) and meet codes up to 8 from the middle, those that meet the
-        # lows have 16 bits; f32: three parts, 24 bits, codes up to 8 from the middle.
+        # Weights times a scale of V are rounded once (bf16 2^-8) and meet codes up to 8 from the middle; so may be those that meet
+        # the middles low + 8 scale, which lie between the values of their group; f32: three parts, 24 bits.
         step_v = max([float(h[2].max()) for h in held[1] if h[2].size] + [0.0])
-        inner = 2.0 ** -8 * 8 * step_v + 2.0 ** -16 * top if self.bf16 else 2.0 ** -22 * 8 * step_v
+        inner = 2.0 ** -8 * (8 * step_v + top) if self.bf16 else 2.0 ** -22 * 8 * step_v
         tol = 2 * score * top + inner + (2.0 ** -8 if self.bf16 else 2.0 ** -22) * np.abs(ref)
         err = np.abs(out - ref)
         assert (err <= tol).all(), float((err / np.maximum(tol, 1e-30)).max())
