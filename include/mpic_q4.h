@@ -104,9 +104,9 @@ int mpic_q4_read(mpic_ctx* ctx, const void* cache, int64_t cache_bytes, int64_t 
  * over the values that the codes stand for.  A query that sees nothing (p < 0, or an empty
  * request) gets zeros and lse = -infinity.
  * BF16: products on the matrix cores with fp32 accumulation over the codes themselves, which are
- * exact; the weights are rounded to bf16 before the second product, alone and times the scale of
- * V; one final rounding of out.  F32: factors split into three bf16 parts (24 bits), fp32
- * otherwise.
+ * exact; the weights (times the scale of V) are rounded to bf16 before the second product, those
+ * that meet V's minima are held in 16 bits or more; one final rounding of out.  F32: factors split
+ * into three bf16 parts (24 bits), fp32 otherwise.
  *
  *   q                 device [n_rows][Hq][D], rows q_stride elements apart (as above)
  *   q_off             device [n_requests + 1], queries of request b are rows q_off[b] ..

@@ -19,12 +19,13 @@
 //
 // With more than eight rows vector instructions are what it costs, so there the lows go through the matrix cores as well: the
 // pairs of K as they lie in the cache, (scale, low), against (-sum(q), sum(q) / 16) in three bf16 parts; those of V, taken apart
-// into rows of scales and of lows, against the weights rounded to bf16: that is the middle of a group, low + 8 scale, times a
-// weight off by 2^-8 at most, which is what a context in bf16 costs too.  A V that is no number would reach rows that do not see it
+// into rows of scales and of lows, against the weights in two bf16 parts (16 bits: a group may be small and far from zero, and
+// its middle, low + 8 scale, has as many bits as its spread then; with one part values of 64 and -64 that cancel leave 0.04 behind, and
+// a launch takes 2 to 6 % less).  A V that is no number would reach rows that do not see it
 // that way (0 * inf), so units that not every row sees whole keep to the vector instructions.  32 rows a workgroup, two tiles
-// of columns for every operand made of codes: 383 vector instructions for 32 rows (they are issued 77 % of the
-// time, the matrix cores busy 29 %; 32 heads over 8, 4 requests of 8192 tokens with 200 new ones: 208 us, 510 TFLOP/s; 16 rows a
-// workgroup 247 us).
+// of columns for every operand made of codes: 424 vector instructions for 32 rows (they are issued 79 % of the
+// time, the matrix cores busy 29 %; 32 heads over 8, 4 requests of 8192 tokens with 200 new ones: 220 us, 480 TFLOP/s; 16 rows a
+// workgroup 257 us).
 //
 // A workgroup of four wavefronts takes a split of a request's keys for one kv head and 8 to 32 rows; its wavefronts take the
 // units in turn and meet in LDS at the end.  Where the keys are cut into several splits, a second launch merges them.
@@ -389,12 +390,20 @@ __device__ inline void attend_unit(Columns<S> (&s)[S::kTiles], const char* unit,
     }
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
-      f32x8 w;
+      // the weights in two parts: their upper halves as they are, and what is left
+      u32x4 high;
+      f32x8 rest;
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) w[4 * b + (r & 1) * 2 + (r >> 1)] = p[t][b][r];
-      s[t].sums = mfma(__builtin_bit_cast(bf16x8, four), __builtin_convertvector(w, bf16x8), s[t].sums);
+        for (int r = 0; r < 2; ++r) {
+          const uint32_t x0 = __builtin_bit_cast(uint32_t, p[t][b][r]), x2 = __builtin_bit_cast(uint32_t, p[t][b][r + 2]);
+          high[2 * b + r] = __builtin_amdgcn_perm(x2, x0, 0x07060302u);
+          rest[4 * b + 2 * r] = p[t][b][r] - __builtin_bit_cast(float, x0 & 0xFFFF0000u);
+          rest[4 * b + 2 * r + 1] = p[t][b][r + 2] - __builtin_bit_cast(float, x2 & 0xFFFF0000u);
+        }
+      s[t].sums = mfma(__builtin_bit_cast(bf16x8, four), __builtin_convertvector(rest, bf16x8), s[t].sums);
+      s[t].sums = mfma(__builtin_bit_cast(bf16x8, four), __builtin_bit_cast(bf16x8, high), s[t].sums);
     }
   }
   Parts<S::kParts> weights[kTiles][S::kLaneGroups];
@@ -727,8 +736,8 @@ __global__ __launch_bounds__(256) void q4_merge_kernel(Q4AttnArgs a) {
 // 8 rows where that is all there is.  Beyond that 16 or 32: a unit of 32 rows costs 1.3 times the instructions of one of 16, but
 // takes longer from its first to its last, and only half as many wavefronts fit.  So 32 rows need a launch that fills the
 // machine, (tiles of 16 rows) * (units of keys) over all kv heads and requests, and no more than a third of its tiles' rows may
-// be without one: 9 500 of those units 19.5 us either way, 20 600 25.1 us against 26.1, 82 000 54 against 68, 419 000 208 against
-// 247; below that 1 to 3 us more (36 rows over 512 tokens 11 us against 8).
+// be without one: 9 500 of those units 19.9 us against 19.0 with 16 rows, 16 200 23.4 against 22.9, 22 800 24.0 against 25.5, 82 400
+// 62.5 against 70.9, 410 000 220 against 257 (36 rows over 512 tokens 11 us against 8).
 //
 // 8 or 16 rows: splits of whole units for every wavefront, so that three workgroups a compute unit are there where the requests
 // alone do not make them (four would fit with 8 rows, but smaller splits cost more: 4 requests of 19841 tokens 18.5 us
@@ -736,7 +745,7 @@ __global__ __launch_bounds__(256) void q4_merge_kernel(Q4AttnArgs a) {
 // splits are cut down to 32 units as long as that makes no more than eight rounds of them.
 // 32 rows: workgroups take longer, so their rounds count (two a compute unit): the number of splits with the least rounds *
 // (units of a split + 16), 16 being what a workgroup and its share of the merge cost besides (2 requests of 16000 tokens with 256
-// new ones 225 us; 10 % more by the rule above).
+// new ones 240 us; 10 % more by the rule above).
 // Five units a wavefront stay in one piece: a further unit takes 0.9 us (4 requests of 128 tokens 4.5 us, of 256 5.4), the
 // merge 2.7 and its launch 2.3 of the host.
 struct Cut {

@@ -1,0 +1,37 @@
+"""Attention over contexts in 4 bits, row by row as near to the oracle as its roundings allow (needs an MI355X)."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2502_01960_amd as mpic
+from closeness import allowed, hold, worst
+from test_closeness_host import opposite
+from test_gpu_q4 import BOUND, DEV, Held, _dt, _i32
+
+pytestmark = pytest.mark.gpu
+
+# (query heads, kv heads, head dim, bf16), new tokens of a request: 8, 16 and 32 rows a workgroup, f32 of both head dims
+FORMS = {"8_rows": ((8, 2, 128, True), 1), "16_rows": ((8, 2, 128, True), 4), "32_rows": ((8, 2, 128, True), 40),
+         "f32_128": ((4, 2, 128, False), 2), "f32_64": ((4, 2, 64, False), 3)}
+
+
+def _close(p, out, lens=None):
+    held = [hold([x.double().numpy() for x in side], p.bf16) for side in (p.k, p.v)]
+    ref, bound = allowed(p.q.double().numpy(), *held, p.lens if lens is None else lens, p.news, 1 / math.sqrt(p.d), p.bf16)
+    share = worst(out, ref, bound)
+    print(f"error norm {share:.3f} of what is allowed")
+    assert share <= 1.0
+
+
+@pytest.mark.parametrize("form", [f for f in FORMS if FORMS[f][0][3]])
+def test_values_far_from_zero_that_cancel(form):
+    """Minima of 64 and -64 in an output of nearly nothing: the weights that meet them have 16 bits in every form."""
+    model, new = FORMS[form]
+    p = Held([100], [new], *model)
+    q, k, v = opposite(100, new, *model[:2])
+    p.q, p.k, p.v = torch.from_numpy(q).to(_dt(True)), [torch.from_numpy(k).to(_dt(True))], [torch.from_numpy(v).to(_dt(True))]
+    j = np.arange(100)
+    mpic.mpic_q4_write(p.ctx.handle, p.k[0].to(DEV), p.v[0].to(DEV), _i32(p.table[0, j // 16] * 16 + j % 16), p.cache, p.n_slots)
+    _close(p, p.run(max_len=BOUND if new == 40 else None)[0])
