@@ -283,13 +283,18 @@ def _ptr(t):
 _torch = None
 
 
-def _stream(stream):
+def _import_torch():
     global _torch
+    if _torch is None:
+        import torch
+        _torch = torch
+    return _torch
+
+
+def _stream(stream):
     if stream is None:
-        if _torch is None:
-            import torch
-            _torch = torch
-        return _torch._C._cuda_getCurrentRawStream(_torch.cuda.current_device())
+        torch = _torch or _import_torch()
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     return getattr(stream, "cuda_stream", stream)
 
 
@@ -425,7 +430,7 @@ def _row_stride(t, shape):
 
 def _int32(t, n, name):
     """Address of a contiguous int32 tensor of n elements."""
-    if t.numel() != n or t.element_size() != 4 or not t.is_contiguous():
+    if t.dtype is not (_torch or _import_torch()).int32 or t.numel() != n or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous int32 tensor of {n} elements")
     return t.data_ptr()
 

@@ -1,0 +1,77 @@
+"""What the binding takes and refuses in front of the calls on positions and contexts in 4 bits (CPU: nothing reaches the GPU)."""
+import pytest
+import torch
+
+import paper_2502_01960_amd as mpic
+from paper_2502_01960_amd import binding
+
+HQ, HKV, D, SLOTS, PAGE = 4, 2, 128, 32, 16
+
+
+class _Taken:
+    """Stands for the library: every call that gets there is noted and does nothing."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        return lambda *a: self.calls.append((name, a)) or 0
+
+
+@pytest.fixture
+def taken(monkeypatch):
+    lib = mpic.load_library()
+    t = _Taken()
+    t.mpic_destroy = lib.mpic_destroy
+    monkeypatch.setattr(binding, "_lib", t)
+    yield t
+    monkeypatch.setattr(binding, "_lib", lib)
+
+
+@pytest.fixture(params=[mpic.MPIC_BF16, mpic.MPIC_F32], ids=["bf16", "f32"])
+def ctx(request):
+    c = mpic.Context(HQ, HKV, D, request.param, 1e4)
+    c.cache_bytes = mpic.mpic_q4_bytes(c.handle, SLOTS)
+    c.torch_dtype = torch.float32 if request.param == mpic.MPIC_F32 else torch.bfloat16
+    return c
+
+
+def _i(*s):
+    return torch.zeros(s, dtype=torch.int32)
+
+
+def _args(ctx, call, n=3, **kw):
+    """(function, arguments) of a call that is right but for what kw replaces."""
+    t = lambda h: torch.zeros((n, h, D), dtype=ctx.torch_dtype)
+    cache = torch.zeros(ctx.cache_bytes, dtype=torch.uint8)
+    a = {"position": lambda: dict(q=t(HQ), k=t(HKV), pos=_i(1, n), q_out=t(HQ), k_out=t(HKV), stream=0),
+         "write": lambda: dict(k=t(HKV), v=t(HKV), slots=_i(n), cache=cache, n_slots=SLOTS, stream=0),
+         "read": lambda: dict(cache=cache, n_slots=SLOTS, slots=_i(n), k=t(HKV), v=t(HKV), stream=0),
+         "attn": lambda: dict(q=t(HQ), cache=cache, n_slots=SLOTS, page_table=_i(n, 2), page_size=PAGE, lens=_i(n), softmax_scale=0.1,
+                              out=t(HQ), stream=0)}[call]()
+    a.update(kw)
+    return {"position": mpic.mpic_position_rows, "write": mpic.mpic_q4_write, "read": mpic.mpic_q4_read, "attn": mpic.mpic_q4_attn}[call], a
+
+
+def _refused(ctx, taken, call, **kw):
+    f, a = _args(ctx, call, **kw)
+    with pytest.raises(ValueError):
+        f(ctx.handle, **a)
+    assert not taken.calls, kw
+
+
+@pytest.mark.parametrize("call", ["position", "write", "read", "attn"])
+def test_calls_that_are_right_arrive(ctx, taken, call):
+    for n in (0, 1, 3):
+        f, a = _args(ctx, call, n=n)
+        f(ctx.handle, **a)
+    assert len(taken.calls) == 3
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.uint32, torch.int64, torch.int16])
+@pytest.mark.parametrize("call,names", [("position", ["pos"]), ("write", ["slots"]), ("read", ["slots"]), ("attn", ["page_table", "lens", "q_off"])])
+def test_what_is_not_int32_is_refused(ctx, taken, call, names, dtype):
+    """A float32 length of 64 would be read as 1115684864."""
+    _, right = _args(ctx, call)
+    for name in names:
+        _refused(ctx, taken, call, **{name: (_i(4) if name == "q_off" else right[name]).to(dtype)})
