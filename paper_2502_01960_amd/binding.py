@@ -423,9 +423,10 @@ def mpic_rank_tokens(dist, n_top):
 def _row_stride(t, shape):
     """Elements from one row to the next of a [rows][heads][D] tensor of that shape whose rows are contiguous."""
     row, head, one = t.stride()
-    if one != 1 or head != shape[2]:
+    n, heads, d = shape
+    if one != 1 or (head != d and heads > 1):     # (the stride of a single head says nothing)
         raise ValueError("expected a [rows][heads][D] tensor with contiguous rows")
-    return row if shape[0] > 1 else head * shape[1]
+    return row if n > 1 else heads * d
 
 
 def _int32(t, n, name):

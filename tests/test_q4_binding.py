@@ -75,3 +75,23 @@ def test_what_is_not_int32_is_refused(ctx, taken, call, names, dtype):
     _, right = _args(ctx, call)
     for name in names:
         _refused(ctx, taken, call, **{name: (_i(4) if name == "q_off" else right[name]).to(dtype)})
+
+
+@pytest.fixture
+def one_head():
+    return mpic.Context(1, 1, D, mpic.MPIC_BF16, 1e4)
+
+
+def test_one_head_may_have_any_stride(one_head, taken):
+    """A contiguous [n][1][D] tensor that was [1][n][D] before: the stride of its only head is that of all rows."""
+    ctx = one_head
+    x = lambda: torch.zeros((1, 5, D), dtype=torch.bfloat16).transpose(0, 1)
+    assert x().is_contiguous() and x().stride(1) == 5 * D
+    cache = torch.zeros(SLOTS * 144, dtype=torch.uint8)
+    mpic.mpic_position_rows(ctx.handle, x(), x(), _i(5), x(), x(), stream=0)
+    mpic.mpic_q4_write(ctx.handle, x(), x(), _i(5), cache, SLOTS, 0)
+    mpic.mpic_q4_read(ctx.handle, cache, SLOTS, _i(5), x(), x(), 0)
+    mpic.mpic_q4_attn(ctx.handle, x(), cache, SLOTS, _i(5, 2), PAGE, _i(5), 0.1, x(), stream=0)
+    assert [name for name, _ in taken.calls] == ["mpic_position_rows", "mpic_q4_write", "mpic_q4_read", "mpic_q4_attn"]
+    strides = [a[i] for (_, a), where in zip(taken.calls, ((2, 4, 13, 15), (2, 4), (7, 9), (2,))) for i in where]
+    assert strides == [D] * len(strides)
