@@ -158,12 +158,24 @@ def _check(rc, ctx=None):
         raise MpicError(rc, mpic_last_error(ctx) if ctx else "")
 
 
+class _Handle(C.c_void_p):
+    """An mpic_ctx that knows what its rows look like: .form = (query heads, kv heads, D, torch type), made when first asked for."""
+
+    def __getattr__(self, name):
+        if name != "form":
+            raise AttributeError(name)
+        torch, c = _import_torch(), self.config
+        self.form = c.n_q_heads, c.n_kv_heads, c.head_dim, torch.bfloat16 if c.dtype == MPIC_BF16 else torch.float32
+        return self.form
+
+
 def mpic_create(n_q_heads, n_kv_heads, head_dim, dtype, rope_theta, rope_interleaved=0, page_size=0,
                 fresh_pre_rope=0, lazy_rope=0):
     cfg = _Config(n_q_heads, n_kv_heads, head_dim, dtype, rope_theta, rope_interleaved, page_size,
                   fresh_pre_rope, lazy_rope)
-    h = C.c_void_p()
+    h = _Handle()
     _check(load_library().mpic_create(C.byref(h), C.byref(cfg)))
+    h.config = cfg
     return h
 
 
@@ -420,10 +432,16 @@ def mpic_rank_tokens(dist, n_top):
 
 
 # The calls below may take the GPU 3 to 5 us, so they look at a tensor no oftener than they have to.
-def _row_stride(t, shape):
-    """Elements from one row to the next of a [rows][heads][D] tensor of that shape whose rows are contiguous."""
+def _form_of(q, k):
+    """The form of a context's rows as they come, for a handle that was not made here."""
+    return q.shape[1], k.shape[1], q.shape[2], q.dtype
+
+
+def _row_stride(t, n, heads, d, dtype):
+    """Elements from one row to the next of a [n][heads][D] tensor of that type whose rows are contiguous."""
+    if t.shape != (n, heads, d) or t.dtype is not dtype:
+        raise ValueError(f"expected a {dtype} tensor [{n}][{heads}][{d}], not {t.dtype} {list(t.shape)}")
     row, head, one = t.stride()
-    n, heads, d = shape
     if one != 1 or (head != d and heads > 1):     # (the stride of a single head says nothing)
         raise ValueError("expected a [rows][heads][D] tensor with contiguous rows")
     return row if n > 1 else heads * d
@@ -439,14 +457,15 @@ def _int32(t, n, name):
 def mpic_position_rows(ctx, q, k, pos, q_out, k_out, q_weight=None, k_weight=None, eps=None, pair_axis=None, stream=None):
     """Norms (eps not None) and rotation of fresh rows: q [n][Hq][D] and k [n][Hkv][D] (rows may be strided) to the positions
     pos [n_axes][n] (or [n]); pair_axis names the axis of every pair.  q_out and k_out may be q and k."""
-    qs, ks = q.shape, k.shape
-    n = qs[0]
+    try:
+        hq, hkv, d, dtype = ctx.form
+    except AttributeError:
+        hq, hkv, d, dtype = _form_of(q, k)
+    n = q.shape[0]
     n_axes = 1 if pos.dim() == 1 else pos.shape[0]
-    if ks[0] != n or q_out.shape != qs or k_out.shape != ks:
-        raise ValueError("q, k, q_out and k_out must have the same rows")
     axis = None
     if pair_axis is not None:
-        if len(pair_axis) != qs[2] // 2:
+        if len(pair_axis) != d // 2:
             raise ValueError("pair_axis must name an axis for each of the D / 2 pairs")
         axis = (C.c_int32 * len(pair_axis))(*pair_axis)
     if eps is None:
@@ -454,9 +473,10 @@ def mpic_position_rows(ctx, q, k, pos, q_out, k_out, q_weight=None, k_weight=Non
     elif eps < 0:
         raise ValueError("eps must not be negative")
     rc = (_lib or load_library()).mpic_position_rows(
-        ctx, q.data_ptr(), _row_stride(q, qs), k.data_ptr(), _row_stride(k, ks), n, _int32(pos, n_axes * n, "pos"), n_axes, axis,
+        ctx, q.data_ptr(), _row_stride(q, n, hq, d, dtype), k.data_ptr(), _row_stride(k, n, hkv, d, dtype), n,
+        _int32(pos, n_axes * n, "pos"), n_axes, axis,
         None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr(), eps,
-        q_out.data_ptr(), _row_stride(q_out, qs), k_out.data_ptr(), _row_stride(k_out, ks), _stream(stream))
+        q_out.data_ptr(), _row_stride(q_out, n, hq, d, dtype), k_out.data_ptr(), _row_stride(k_out, n, hkv, d, dtype), _stream(stream))
     if rc:
         _check(rc, ctx)
 
@@ -476,12 +496,13 @@ def _cache_bytes(cache):
 
 def mpic_q4_write(ctx, k, v, slots, cache, n_slots, stream=None):
     """Row r of k and v ([n][Hkv][D], rows may be strided) goes to slot slots[r] (None: slot r) of the cache."""
-    shape = k.shape
-    if v.shape != shape:
-        raise ValueError("k and v must have the same shape")
-    n = shape[0]
+    try:
+        _, heads, d, dtype = ctx.form
+    except AttributeError:
+        _, heads, d, dtype = _form_of(k, k)
+    n = k.shape[0]
     rc = (_lib or load_library()).mpic_q4_write(
-        ctx, k.data_ptr(), _row_stride(k, shape), v.data_ptr(), _row_stride(v, shape), n,
+        ctx, k.data_ptr(), _row_stride(k, n, heads, d, dtype), v.data_ptr(), _row_stride(v, n, heads, d, dtype), n,
         None if slots is None else _int32(slots, n, "slots"), cache.data_ptr(), _cache_bytes(cache), n_slots, _stream(stream))
     if rc:
         _check(rc, ctx)
@@ -489,13 +510,14 @@ def mpic_q4_write(ctx, k, v, slots, cache, n_slots, stream=None):
 
 def mpic_q4_read(ctx, cache, n_slots, slots, k, v, stream=None):
     """Rows of k and v = the values that the slots hold; rows without a slot in the cache are left as they were."""
-    shape = k.shape
-    if v.shape != shape:
-        raise ValueError("k and v must have the same shape")
-    n = shape[0]
+    try:
+        _, heads, d, dtype = ctx.form
+    except AttributeError:
+        _, heads, d, dtype = _form_of(k, k)
+    n = k.shape[0]
     rc = (_lib or load_library()).mpic_q4_read(
         ctx, cache.data_ptr(), _cache_bytes(cache), n_slots, None if slots is None else _int32(slots, n, "slots"), n, k.data_ptr(),
-        _row_stride(k, shape), v.data_ptr(), _row_stride(v, shape), _stream(stream))
+        _row_stride(k, n, heads, d, dtype), v.data_ptr(), _row_stride(v, n, heads, d, dtype), _stream(stream))
     if rc:
         _check(rc, ctx)
 
@@ -512,14 +534,18 @@ def mpic_q4_attn(ctx, q, cache, n_slots, page_table, page_size, lens, softmax_sc
     """Attention over contexts in 4 bits: q [n_rows][Hq][D] (rows may be strided), page_table [B][width], lens [B], with
     several queries per request q_off [B + 1]; all of them int32 device tensors.  workspace: a device tensor of
     mpic_q4_attn_workspace bytes."""
+    try:
+        heads, _, d, dtype = ctx.form
+    except AttributeError:
+        heads, _, d, dtype = _form_of(q, q)
     shape, (b, width) = q.shape, page_table.shape
     n = shape[0]
-    if out.shape != shape or not out.is_contiguous():
+    if out.shape != shape or out.dtype is not dtype or not out.is_contiguous():
         raise ValueError("out must be contiguous and like q")
-    if lse is not None and (lse.numel() != n * shape[1] or lse.element_size() != 4 or not lse.is_contiguous()):
+    if lse is not None and (lse.numel() != n * heads or lse.dtype is not (_torch or _import_torch()).float32 or not lse.is_contiguous()):
         raise ValueError("lse must be a contiguous float32 [n_rows][Hq] tensor")
     rc = (_lib or load_library()).mpic_q4_attn(
-        ctx, q.data_ptr(), _row_stride(q, shape), n, None if q_off is None else _int32(q_off, b + 1, "q_off"), max_q,
+        ctx, q.data_ptr(), _row_stride(q, n, heads, d, dtype), n, None if q_off is None else _int32(q_off, b + 1, "q_off"), max_q,
         cache.data_ptr(), _cache_bytes(cache), n_slots, _int32(page_table, b * width, "page_table"), width, page_size,
         _int32(lens, b, "lens"), b, width * page_size if max_len is None else max_len, softmax_scale, out.data_ptr(),
         None if lse is None else lse.data_ptr(), None if workspace is None else workspace.data_ptr(),

@@ -95,3 +95,47 @@ def test_one_head_may_have_any_stride(one_head, taken):
     assert [name for name, _ in taken.calls] == ["mpic_position_rows", "mpic_q4_write", "mpic_q4_read", "mpic_q4_attn"]
     strides = [a[i] for (_, a), where in zip(taken.calls, ((2, 4, 13, 15), (2, 4), (7, 9), (2,))) for i in where]
     assert strides == [D] * len(strides)
+
+
+def _rows_of(call):
+    return {"position": (("q", HQ), ("k", HKV), ("q_out", HQ), ("k_out", HKV)), "write": (("k", HKV), ("v", HKV)),
+            "read": (("k", HKV), ("v", HKV)), "attn": (("q", HQ), ("out", HQ))}[call]
+
+
+@pytest.mark.parametrize("call", ["position", "write", "read", "attn"])
+def test_rows_of_another_type_or_form_are_refused(ctx, taken, call):
+    """A bf16 output of an f32 context would be written to twice its size; rows of a projection with fewer heads than the
+    context's take the next part of the row along."""
+    other = torch.float32 if ctx.torch_dtype == torch.bfloat16 else torch.bfloat16
+    for name, heads in _rows_of(call):
+        t = lambda h=heads, n=3, d=D, dt=ctx.torch_dtype: torch.zeros((n, h, d), dtype=dt)
+        wide = torch.zeros((3, 8, D), dtype=ctx.torch_dtype)
+        bad = [t(dt=other), t(dt=torch.float16), t(h=heads - 1), t(h=heads + 1), t(d=D // 2), t(d=2 * D)]
+        if name != "out":
+            bad += [wide[:, :heads - 1], wide[:, :heads + 1]]
+        if name not in ("q", "k") or (call, name) == ("position", "k"):
+            bad += [t(n=2), t(n=4)]
+        for x in bad:
+            _refused(ctx, taken, call, **{name: x})
+    if call == "attn":           # q and out alike, and unlike the context
+        for h in (2, 8):
+            x = torch.zeros((3, h, D), dtype=ctx.torch_dtype)
+            _refused(ctx, taken, call, q=x, out=x.clone())
+        for lse in (torch.zeros((3, HQ), dtype=torch.int32), torch.zeros((3, HQ), dtype=torch.float64), torch.zeros((3, HQ + 1))):
+            _refused(ctx, taken, call, lse=lse)
+        f, a = _args(ctx, call, lse=torch.zeros((3, HQ)))
+        f(ctx.handle, **a)
+
+
+def test_a_handle_that_was_made_elsewhere_serves_as_before(ctx, taken):
+    """Its form is not known, so rows only have to agree among themselves."""
+    import ctypes
+    for call in ("position", "write", "read", "attn"):
+        f, a = _args(ctx, call)
+        f(ctypes.c_void_p(ctx.handle.value), **a)
+        f(ctx.handle.value, **a)
+        name, heads = _rows_of(call)[-1]
+        f, a = _args(ctx, call, **{name: torch.zeros((3, heads + 1, D + 1), dtype=ctx.torch_dtype)})
+        with pytest.raises(ValueError):
+            f(ctx.handle.value, **a)
+    assert len(taken.calls) == 8
