@@ -454,6 +454,15 @@ def _int32(t, n, name):
     return t.data_ptr()
 
 
+def _weight(t, d, dtype):
+    """Address of a norm's weights; None: all ones."""
+    if t is None:
+        return None
+    if t.shape != (d,) or t.dtype is not dtype or not t.is_contiguous():
+        raise ValueError(f"weights of a norm must be a contiguous {dtype} tensor [{d}]")
+    return t.data_ptr()
+
+
 def mpic_position_rows(ctx, q, k, pos, q_out, k_out, q_weight=None, k_weight=None, eps=None, pair_axis=None, stream=None):
     """Norms (eps not None) and rotation of fresh rows: q [n][Hq][D] and k [n][Hkv][D] (rows may be strided) to the positions
     pos [n_axes][n] (or [n]); pair_axis names the axis of every pair.  q_out and k_out may be q and k."""
@@ -475,7 +484,7 @@ def mpic_position_rows(ctx, q, k, pos, q_out, k_out, q_weight=None, k_weight=Non
     rc = (_lib or load_library()).mpic_position_rows(
         ctx, q.data_ptr(), _row_stride(q, n, hq, d, dtype), k.data_ptr(), _row_stride(k, n, hkv, d, dtype), n,
         _int32(pos, n_axes * n, "pos"), n_axes, axis,
-        None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr(), eps,
+        _weight(q_weight, d, dtype), _weight(k_weight, d, dtype), eps,
         q_out.data_ptr(), _row_stride(q_out, n, hq, d, dtype), k_out.data_ptr(), _row_stride(k_out, n, hkv, d, dtype), _stream(stream))
     if rc:
         _check(rc, ctx)
