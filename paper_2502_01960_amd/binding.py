@@ -458,8 +458,8 @@ def _weight(t, d, dtype):
     """Address of a norm's weights; None: all ones."""
     if t is None:
         return None
-    if t.shape != (d,) or t.dtype is not dtype or not t.is_contiguous():
-        raise ValueError(f"weights of a norm must be a contiguous {dtype} tensor [{d}]")
+    if t.numel() != d or t.dtype is not dtype or not t.is_contiguous():
+        raise ValueError(f"weights of a norm must be a contiguous {dtype} tensor of {d} elements")
     return t.data_ptr()
 
 

@@ -145,10 +145,10 @@ def test_weights_of_another_type_or_length_are_refused(ctx, taken):
     """f32 weights of a bf16 context would be read as bf16, short ones past their end, strided ones between their values."""
     other = torch.float32 if ctx.torch_dtype == torch.bfloat16 else torch.bfloat16
     w = torch.zeros(D, dtype=ctx.torch_dtype)
-    for bad in (w.to(other), w[:D // 2], w[:D - 1], torch.zeros(D + 1, dtype=ctx.torch_dtype), w[None], torch.zeros(2 * D, dtype=ctx.torch_dtype)[::2]):
+    for bad in (w.to(other), w[:D // 2], w[:D - 1], torch.zeros(D + 1, dtype=ctx.torch_dtype), torch.zeros(2 * D, dtype=ctx.torch_dtype)[::2]):
         for name in ("q_weight", "k_weight"):
             _refused(ctx, taken, "position", eps=1e-6, **{name: bad})
-    for kw in (dict(q_weight=w, k_weight=w), dict(q_weight=w), dict(k_weight=w), {}):
+    for kw in (dict(q_weight=w, k_weight=w), dict(q_weight=w), dict(k_weight=w[None]), {}):
         f, a = _args(ctx, "position", eps=1e-6, **kw)
         f(ctx.handle, **a)
     assert len(taken.calls) == 4
