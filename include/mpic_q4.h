@@ -122,6 +122,7 @@ int mpic_q4_read(mpic_ctx* ctx, const void* cache, int64_t cache_bytes, int64_t 
  *   lens              device [n_requests]; negative = 0, more than max_len = max_len
  *   max_len           bound on lens, 0 .. table_width * page_size (shapes the launch: a bound near
  *                     the lengths makes it faster)
+ *   softmax_scale     2^-126 .. 2^123
  *   out               device [n_rows][Hq][D]
  *   lse               device float [n_rows][Hq]; may be NULL
  *   workspace         device, 16-byte aligned, at least mpic_q4_attn_workspace bytes for the same

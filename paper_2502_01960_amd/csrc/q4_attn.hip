@@ -845,7 +845,8 @@ extern "C" int mpic_q4_attn(mpic_ctx* ctx, const void* q, int64_t q_stride, int6
   if (page_size <= 0 || page_size % q4::kTokens) return invalid("q4_attn: page_size must be a positive multiple of 16");
   if (table_width < 0 || table_width > INT32_MAX || max_len > table_width * page_size) return invalid("q4_attn: page table narrower than max_len");
   if (n_slots < 0 || n_slots >= INT32_MAX) return invalid("q4_attn: bad slot count");
-  if (!(softmax_scale > 0.0) || !std::isfinite(softmax_scale)) return invalid("q4_attn: softmax_scale must be finite and positive");
+  // (16 log2(e) times it is an fp32 number that is neither zero, which a masked -inf would make no number, nor infinite)
+  if (!(softmax_scale >= 0x1p-126 && softmax_scale <= 0x1p123)) return invalid("q4_attn: softmax_scale must be positive, 2^-126 to 2^123");
   if (q_stride < static_cast<int64_t>(c.n_q_heads) * c.head_dim || q_stride * elem % 16)
     return invalid("q4_attn: q_stride must hold a row and be a multiple of 16 bytes");
   if (cache_bytes < q4::cache_bytes(c.dtype == MPIC_F32, c.head_dim, c.n_kv_heads, n_slots)) return invalid("q4_attn: the cache is smaller than its slots");

@@ -8,7 +8,7 @@ import torch
 import paper_2502_01960_amd as mpic
 from closeness import allowed, hold, worst
 from test_closeness_host import opposite
-from test_gpu_q4 import BOUND, DEV, Held, _dt, _i32
+from test_gpu_q4 import BOUND, DEV, Held, _attend, _dt, _i32
 
 pytestmark = pytest.mark.gpu
 
@@ -17,9 +17,9 @@ FORMS = {"8_rows": ((8, 2, 128, True), 1), "16_rows": ((8, 2, 128, True), 4), "3
          "f32_128": ((4, 2, 128, False), 2), "f32_64": ((4, 2, 64, False), 3)}
 
 
-def _close(p, out, lens=None):
+def _close(p, out, lens=None, scale=None):
     held = [hold([x.double().numpy() for x in side], p.bf16) for side in (p.k, p.v)]
-    ref, bound = allowed(p.q.double().numpy(), *held, p.lens if lens is None else lens, p.news, 1 / math.sqrt(p.d), p.bf16)
+    ref, bound = allowed(p.q.double().numpy(), *held, p.lens if lens is None else lens, p.news, scale or 1 / math.sqrt(p.d), p.bf16)
     share = worst(out, ref, bound)
     print(f"error norm {share:.3f} of what is allowed")
     assert share <= 1.0
@@ -35,3 +35,16 @@ def test_values_far_from_zero_that_cancel(form):
     j = np.arange(100)
     mpic.mpic_q4_write(p.ctx.handle, p.k[0].to(DEV), p.v[0].to(DEV), _i32(p.table[0, j // 16] * 16 + j % 16), p.cache, p.n_slots)
     _close(p, p.run(max_len=BOUND if new == 40 else None)[0])
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_the_least_scale_weighs_all_tokens_alike(form):
+    """Some of which are not seen."""
+    model, new = FORMS[form]
+    p = Held([90, 33], [new, 2], *model)
+    out = torch.full(p.q.shape, 77.0, dtype=_dt(p.bf16), device=DEV)
+    bound = BOUND if new == 40 else p.table.shape[1] * p.page
+    table = np.pad(p.table, ((0, 0), (0, bound // p.page - p.table.shape[1])), constant_values=-1)
+    _attend(p.ctx, p.q.to(DEV), p.cache, p.n_slots, _i32(table), p.page, _i32(p.lens), out, None, _i32(p.q_off), max(p.news), bound,
+            2.0 ** -126)
+    _close(p, out.double().cpu().numpy(), scale=2.0 ** -126)

@@ -1,0 +1,13 @@
+"""What the entry points for positions and contexts in 4 bits refuse at the ends of their ranges (CPU: nothing reaches the GPU)."""
+
+import paper_2502_01960_amd as mpic
+from test_q4_host import A, INVALID, _attn, ctx    # noqa: F401
+
+
+def test_scales_that_are_no_positive_fp32_number_are_refused(ctx):
+    """1e-60 is zero in fp32, and zero times the -infinity of a token that is not seen is no number."""
+    for scale in (1e-60, 1e-300, 5e-324, 2.0 ** -127, 2.0 ** 124, 1e38, 1e300):
+        assert _attn(ctx, scale=scale) == INVALID, scale
+        assert "softmax_scale" in mpic.binding.mpic_last_error(ctx.handle)
+    for scale in (2.0 ** -126, 2.0 ** 123):
+        assert _attn(ctx, scale=scale, n_rows=0, q_off=A, q=None, out=None) == 0, scale
