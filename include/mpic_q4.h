@@ -34,8 +34,14 @@ extern "C" {
  *
  * With several axes (rows of images and videos: time, height, width) each pair follows one
  * of them.  A stored chunk whose rows were positioned this way, counted from its own
- * origin, is moved by the same distance on every axis when all axes of its first token
- * advance alike, which is the shift that mpic_assemble_kv applies.
+ * origin, is moved by the same distance on every axis, and the distance that
+ * mpic_assemble_kv moves it by is the token index of its first token in the request.  So
+ * a chunk of several axes may be linked only where its origin lies at that index on all
+ * axes, and the fresh rows around it have to be positioned by the same count.  Models
+ * whose positions go on by less than a chunk's tokens behind it (by 24 behind an image of
+ * 24 x 24) do not link so, and nothing in the rows tells: no plan gives another distance.
+ * Their stored keys are turned by the difference first, on every axis: this call without
+ * norms, positions = wanted origin - token index, negative or not, and one rounding more.
  *
  *   q [n_rows][Hq][D], k [n_rows][Hkv][D]  device, rows q_stride / k_stride elements apart
  *                     (so both may be parts of the rows of one projection): multiples of 16
