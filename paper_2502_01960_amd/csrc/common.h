@@ -202,8 +202,11 @@ struct mpic_plan {
 
 namespace mpic {
 
+// Set the context's error message and return the code.  With plain text ("what" or "what: why") and from fail_hip nothing
+// is thrown: without host memory for the message there is none, and the code is what counts.
+int fail(mpic_ctx* ctx, int code, const char* what, const char* why = nullptr) noexcept;
 int fail(mpic_ctx* ctx, int code, const std::string& msg);
-int fail_hip(mpic_ctx* ctx, hipError_t e, const char* what);
+int fail_hip(mpic_ctx* ctx, hipError_t e, const char* what) noexcept;
 
 #define MPIC_HIP(ctx, call)                                  \
   do {                                                       \

@@ -22,10 +22,17 @@ int fail(mpic_ctx* ctx, int code, const std::string& msg) {
   return code;
 }
 
-int fail_hip(mpic_ctx* ctx, hipError_t e, const char* what) {
-  if (ctx) ctx->last_error = std::string(what) + ": " + hipGetErrorString(e);
-  return MPIC_ERR_HIP;
+int fail(mpic_ctx* ctx, int code, const char* what, const char* why) noexcept {
+  if (ctx) try {
+      ctx->last_error = what;
+      if (why) ctx->last_error.append(": ").append(why);
+    } catch (const std::bad_alloc&) {
+      ctx->last_error.clear();
+    }
+  return code;
 }
+
+int fail_hip(mpic_ctx* ctx, hipError_t e, const char* what) noexcept { return fail(ctx, MPIC_ERR_HIP, what, hipGetErrorString(e)); }
 
 namespace {
 

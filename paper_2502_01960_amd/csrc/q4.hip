@@ -419,7 +419,7 @@ __global__ __launch_bounds__(256) void q4_read_kernel(RowsArgs a) {
 int rows_args(mpic_ctx* ctx, const char* what, const void* k, int64_t k_stride, const void* v, int64_t v_stride, int64_t n_rows,
               const int32_t* slots, const void* cache, int64_t cache_bytes, int64_t n_slots, RowsArgs* a, bool* go) {
   const mpic_config& c = ctx->cfg;
-  const auto invalid = [&](const char* why) { return fail(ctx, MPIC_ERR_INVALID, std::string(what) + ": " + why); };
+  const auto invalid = [&](const char* why) { return fail(ctx, MPIC_ERR_INVALID, what, why); };
   const int64_t elem = c.dtype == MPIC_F32 ? 4 : 2, row = static_cast<int64_t>(c.n_kv_heads) * c.head_dim;
   *go = false;
   if (n_rows < 0 || n_rows >= INT32_MAX) return invalid("bad row count");
@@ -433,7 +433,7 @@ int rows_args(mpic_ctx* ctx, const char* what, const void* k, int64_t k_stride, 
   if ((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v) | reinterpret_cast<uintptr_t>(cache)) & 15)
     return invalid("buffers must be 16-byte aligned");
   if ((n_rows + kTokens - 1) / kTokens * c.n_kv_heads * 2 > INT32_MAX / 64)  // (wavefronts; threads of a launch)
-    return fail(ctx, MPIC_ERR_UNSUPPORTED, std::string(what) + ": too many rows and heads for one launch");
+    return fail(ctx, MPIC_ERR_UNSUPPORTED, what, "too many rows and heads for one launch");
   const int rc = bind_device(ctx);
   if (rc != MPIC_OK) return rc;
   a->k = static_cast<const char*>(k);

@@ -1,7 +1,12 @@
 """What the entry points for positions and contexts in 4 bits refuse at the ends of their ranges (CPU: nothing reaches the GPU)."""
+import os
+import shutil
+import subprocess
+
+import pytest
 
 import paper_2502_01960_amd as mpic
-from test_q4_host import A, INVALID, _attn, ctx    # noqa: F401
+from test_q4_host import A, INVALID, _attn, ROOT, ctx    # noqa: F401
 
 
 def test_scales_that_are_no_positive_fp32_number_are_refused(ctx):
@@ -11,3 +16,13 @@ def test_scales_that_are_no_positive_fp32_number_are_refused(ctx):
         assert "softmax_scale" in mpic.binding.mpic_last_error(ctx.handle)
     for scale in (2.0 ** -126, 2.0 ** 123):
         assert _attn(ctx, scale=scale, n_rows=0, q_off=A, q=None, out=None) == 0, scale
+
+
+@pytest.mark.skipif(shutil.which("g++") is None, reason="needs g++")
+def test_refusals_without_host_memory_throw_nothing(tmp_path):
+    exe = str(tmp_path / "q4_no_memory")
+    lib = mpic.lib_path()
+    subprocess.run(["g++", "-std=c++17", "-O1", "-rdynamic", "-I", os.path.join(ROOT, "include"), os.path.join(ROOT, "tests", "native", "q4_no_memory.cpp"),
+                    lib, "-Wl,-rpath," + os.path.dirname(lib), "-o", exe], check=True, capture_output=True, text=True, timeout=300)
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "refused without memory" in r.stdout, r.stdout + r.stderr
