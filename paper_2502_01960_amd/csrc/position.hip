@@ -120,16 +120,23 @@ __global__ __launch_bounds__(256) void position_kernel(PositionArgs a, int heads
   }
 }
 
+// Workgroups and heads of a wavefront.  Few rows: their heads are spread over more wavefronts.
+struct Spread {
+  int64_t blocks, parts;
+  int heads;
+};
+Spread spread_of(int64_t n_rows, int64_t n_heads, int head_bytes) {
+  const int at_a_time = 64 / (head_bytes / 32);
+  const int64_t blocks = (n_rows + 3) / 4, steps = (n_heads + at_a_time - 1) / at_a_time;
+  const int64_t per_part = blocks >= 1024 ? steps : 1;
+  return {blocks, (steps + per_part - 1) / per_part, static_cast<int>(per_part * at_a_time)};
+}
+
 template <typename T, int D>
 void launch_position(const PositionArgs& a, bool interleaved, bool norm, hipStream_t stream) {
-  constexpr int kHeads = 64 / (D * static_cast<int>(sizeof(T)) / 32);
-  // Few rows: their heads are spread over more wavefronts
-  const int64_t blocks = (a.n_rows + 3) / 4;
-  const int steps = (a.n_heads + kHeads - 1) / kHeads;
-  const int per_part = blocks >= 1024 ? steps : 1;
-  const int parts = (steps + per_part - 1) / per_part;
-  const dim3 grid(static_cast<unsigned>(blocks), static_cast<unsigned>(parts));
-  const int heads = per_part * kHeads;
+  const Spread s = spread_of(a.n_rows, a.n_heads, D * static_cast<int>(sizeof(T)));
+  const dim3 grid(static_cast<unsigned>(s.blocks), static_cast<unsigned>(s.parts));
+  const int heads = s.heads;
   auto go = [&](auto i, auto n) {
     hipLaunchKernelGGL((position_kernel<T, D, decltype(i)::value, decltype(n)::value>), grid, dim3(256), 0, stream, a, heads);
   };
@@ -179,7 +186,10 @@ extern "C" int mpic_position_rows(mpic_ctx* ctx, const void* q, int64_t q_stride
     return fail(ctx, MPIC_ERR_INVALID, "position_rows: buffers must be 16-byte aligned");
   if ((q == q_out && q_stride != q_out_stride) || (k == k_out && k_stride != k_out_stride))
     return fail(ctx, MPIC_ERR_INVALID, "position_rows: rows positioned in place must keep their stride");
-  if (n_rows > INT32_MAX / 64) return fail(ctx, MPIC_ERR_UNSUPPORTED, "position_rows: too many rows for one launch");  // (threads of a launch)
+  // (threads of a launch, its second dimension, head counts in the kernel)
+  const int64_t n_heads = static_cast<int64_t>(c.n_q_heads) + c.n_kv_heads;
+  if (n_rows > INT32_MAX / 64 || n_heads > INT32_MAX / 128 || spread_of(n_rows, n_heads, c.head_dim * (c.dtype == MPIC_F32 ? 4 : 2)).parts > 65535)
+    return fail(ctx, MPIC_ERR_UNSUPPORTED, "position_rows: too many rows or heads for one launch");
   const int rc = bind_device(ctx);
   if (rc != MPIC_OK) return rc;
   if (!ctx->turns_known) {

@@ -6,7 +6,7 @@ import subprocess
 import pytest
 
 import paper_2502_01960_amd as mpic
-from test_q4_host import A, INVALID, _attn, ROOT, ctx    # noqa: F401
+from test_q4_host import A, INVALID, ROOT, UNSUPPORTED, _attn, _position, ctx    # noqa: F401
 
 
 def test_scales_that_are_no_positive_fp32_number_are_refused(ctx):
@@ -26,3 +26,13 @@ def test_refusals_without_host_memory_throw_nothing(tmp_path):
                     lib, "-Wl,-rpath," + os.path.dirname(lib), "-o", exe], check=True, capture_output=True, text=True, timeout=300)
     r = subprocess.run([exe], capture_output=True, text=True, timeout=300)
     assert r.returncode == 0 and "refused without memory" in r.stdout, r.stdout + r.stderr
+
+
+@pytest.mark.parametrize("dtype,heads", [(mpic.MPIC_BF16, 8 * 65535), (mpic.MPIC_F32, 4 * 65535)])
+def test_more_heads_than_a_launch_holds_are_refused(dtype, heads):
+    """Few rows spread their heads over the grid's second dimension, 65535 workgroups of 8 heads (f32: 4)."""
+    wide = mpic.Context(heads, 1, 128, dtype, 1e4)      # (and one of k)
+    row = heads * 128
+    assert _position(wide, q_stride=row, qo_stride=row) == UNSUPPORTED
+    assert "position_rows" in mpic.binding.mpic_last_error(wide.handle)
+    assert _position(wide, q_stride=row, qo_stride=row, n=0) == 0
