@@ -74,6 +74,7 @@ int mpic_position_rows(mpic_ctx* ctx, const void* q, int64_t q_stride, const voi
  * So the least value of a group is held exactly and no value is off by more than half a
  * scale and the rounding of the scale (times the code).  A group with a value that is not
  * finite, or whose range overflows fp32, stands for 64 NaN.
+ * Errors: MPIC_ERR_INVALID, MPIC_ERR_UNSUPPORTED (more bytes than 64 bits hold).
  */
 int mpic_q4_bytes(const mpic_ctx* ctx, int64_t n_slots, int64_t* bytes);
 

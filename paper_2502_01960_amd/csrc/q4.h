@@ -39,8 +39,11 @@ struct Block {
 inline int64_t block_bytes(bool f32, int head_dim) {
   return f32 ? (head_dim == 128 ? Block<float, 128>::kBytes : Block<float, 64>::kBytes) : Block<__bf16, 128>::kBytes;
 }
+// INT64_MAX (which no cache has) for what 64 bits do not hold
 inline int64_t cache_bytes(bool f32, int head_dim, int n_kv_heads, int64_t n_slots) {
-  return (n_slots + kTokens - 1) / kTokens * n_kv_heads * block_bytes(f32, head_dim);
+  int64_t bytes = (n_slots + kTokens - 1) / kTokens;
+  if (__builtin_mul_overflow(bytes, static_cast<int64_t>(n_kv_heads), &bytes) || __builtin_mul_overflow(bytes, block_bytes(f32, head_dim), &bytes)) return INT64_MAX;
+  return bytes;
 }
 
 }  // namespace q4

@@ -455,7 +455,9 @@ int rows_args(mpic_ctx* ctx, const char* what, const void* k, int64_t k_stride, 
 extern "C" int mpic_q4_bytes(const mpic_ctx* ctx, int64_t n_slots, int64_t* bytes) {
   if (!ctx || !bytes || n_slots < 0 || n_slots >= INT32_MAX) return MPIC_ERR_INVALID;
   const mpic_config& c = ctx->cfg;
-  *bytes = mpic::q4::cache_bytes(c.dtype == MPIC_F32, c.head_dim, c.n_kv_heads, n_slots);
+  const int64_t need = mpic::q4::cache_bytes(c.dtype == MPIC_F32, c.head_dim, c.n_kv_heads, n_slots);
+  if (need == INT64_MAX) return MPIC_ERR_UNSUPPORTED;
+  *bytes = need;
   return MPIC_OK;
 }
 
