@@ -48,3 +48,24 @@ def test_the_least_scale_weighs_all_tokens_alike(form):
     _attend(p.ctx, p.q.to(DEV), p.cache, p.n_slots, _i32(table), p.page, _i32(p.lens), out, None, _i32(p.q_off), max(p.news), bound,
             2.0 ** -126)
     _close(p, out.double().cpu().numpy(), scale=2.0 ** -126)
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("n", [2000, 4000, 9000])
+def test_splits_and_their_merge(form, n):
+    """Up to 8 splits, up to 16, more: the merge has a shape for each."""
+    model, new = FORMS[form]
+    p = Held([n, n // 2 + 1, 2], [new, new, 1], *model, page=64)
+    for max_len in (None, 3 * n):
+        _close(p, p.run(max_len=max_len)[0])
+    if new == 40:
+        _close(p, p.run(max_len=BOUND)[0])
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("n", [1, 2, 16, 33, 130, 500])
+def test_short_contexts(form, n):
+    model, new = FORMS[form]
+    p = Held([n, 3], [new, 1], *model, page=16)
+    _close(p, p.run()[0])
+    _close(p, p.run(max_len=BOUND)[0])
