@@ -69,3 +69,13 @@ def test_short_contexts(form, n):
     p = Held([n, 3], [new, 1], *model, page=16)
     _close(p, p.run()[0])
     _close(p, p.run(max_len=BOUND)[0])
+
+
+@pytest.mark.parametrize("form", [f for f in FORMS if f != "32_rows"])
+def test_pages_are_looked_up_again_behind_32_units_of_a_wavefront(form):
+    """A launch of so many requests that a split has 53 units for every wavefront; one request has keys for two and a half of
+    them, in shuffled pages."""
+    model, new = FORMS[form]
+    lens, news = [14000] + [0, 1, 40, 0, 0, 2, 0] * 146 + [300], [new] + [1] * 1023
+    p = Held(lens, news, *model, page=64)
+    _close(p, p.run(max_len=20000)[0])
