@@ -79,3 +79,21 @@ def test_pages_are_looked_up_again_behind_32_units_of_a_wavefront(form):
     lens, news = [14000] + [0, 1, 40, 0, 0, 2, 0] * 146 + [300], [new] + [1] * 1023
     p = Held(lens, news, *model, page=64)
     _close(p, p.run(max_len=20000)[0])
+
+
+def test_requests_that_are_shifted_or_cut_by_their_offsets():
+    """Rows of no request are left as they were, the others are right: offsets that leave rows in front and behind, that are
+    cut to the rows there are, that run backwards (a request without queries)."""
+    p = Held([64, 64, 33], [2, 2, 1], 4, 2, 128, True)
+    every = p.q
+    for off, rows in (([2, 5, 5, 5], {0: (2, 3)}), ([1, 1, 3, 3], {1: (1, 2)}), ([0, 9, 1, 0], {0: (0, 5)}),
+                      ([-9, 1, 2 ** 31 - 1, 7], {0: (0, 1), 1: (1, 4)}), ([4, 1, 0, 0], {}), ([3, 2, 5, 4], {1: (2, 3)})):
+        p.q, p.q_off = every, np.array(off)
+        out, lse = p.run(max_q=5)
+        told = np.zeros(len(every), bool)
+        for b, (first, n) in rows.items():
+            told[first:first + n] = True
+            one = Held([1], [1], 4, 2, 128, True)
+            one.k, one.v, one.q, one.lens, one.news = [p.k[b]], [p.v[b]], every[first:first + n], [p.lens[b]], [n]
+            _close(one, out[first:first + n])
+        assert (out[~told] == 77).all() and (lse[~told] == 77).all(), off
