@@ -32,7 +32,6 @@ struct PositionArgs {
   int64_t n_rows, q_stride, k_stride, q_out_stride, k_out_stride;  // strides in elements
   int32_t n_q_heads, n_heads;                                      // query heads, query and key heads
   float eps;
-  int32_t n_axes;
   uint64_t axis_bits[2];        // two bits a pair
   uint64_t turn[kMaxPairs];     // F_i
 };
@@ -216,7 +215,6 @@ extern "C" int mpic_position_rows(mpic_ctx* ctx, const void* q, int64_t q_stride
   a.n_q_heads = c.n_q_heads;
   a.n_heads = c.n_q_heads + c.n_kv_heads;
   a.eps = eps > 0 ? std::max(static_cast<float>(eps), FLT_MIN) : 0.f;  // (zeros stay zeros however small it is)
-  a.n_axes = n_axes;
   hipStream_t stream = static_cast<hipStream_t>(stream_);
   const bool norm = eps >= 0, inter = c.rope_interleaved != 0;
   if (c.dtype == MPIC_BF16)

@@ -18,8 +18,6 @@ using q4::Block;
 using q4::kGroup;
 using q4::kTokens;
 
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-
 struct RowsArgs {
   const char* k;  // rows (read or written)
   const char* v;

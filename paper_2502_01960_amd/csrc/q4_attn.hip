@@ -520,7 +520,7 @@ __global__ __launch_bounds__(kWaves * 64, kWavesPerSimd) void q4_attn_kernel(Q4A
   };
   char* ring = lds + wave * L::kWave;
   const uint32_t ring_lds = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(MPIC_LDS_PTR(char, ring)));
-  // load unit i of this wavefront into its half of the ring; bit b of the result: block b is in the cache
+  // load unit i of this wavefront into the next place of its ring; bit b of the result: block b is in the cache
   int ring_at = 0;  // of unit i to be staged
   auto stage = [&](int i) {
     if ((i & 31) == 0) look_up(i);
