@@ -54,6 +54,8 @@ extern "C" {
  *   q_out, k_out      device, like q and k.  May be q and k themselves with the same strides;
  *                     must not overlap them otherwise
  * A row of zeros stays zeros for eps > 0; with eps = 0 it becomes NaN, as the formula says.
+ * Squares are fp32: a head whose sum of squares passes 2^128 becomes zeros, and squares below
+ * 2^-149 are zero.
  * Errors: MPIC_ERR_INVALID, MPIC_ERR_UNSUPPORTED (launch beyond the grid's limits), MPIC_ERR_HIP.
  */
 int mpic_position_rows(mpic_ctx* ctx, const void* q, int64_t q_stride, const void* k, int64_t k_stride,

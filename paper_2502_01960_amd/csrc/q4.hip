@@ -6,7 +6,8 @@
 // arranged as the codes are: its 64 lanes hold the codes of 16 tokens, and what a group of 64 values shares is found by
 // exchanges between 4 lanes (K) or 16 (V).  Rows come and go with streaming loads and stores (79360 rows of 4 heads, written and
 // read back: 83 us, 92 with ordinary ones); codes are stored the ordinary way, streaming stores take 15 us more.  Writing
-// takes 49 us of that (4.3 TB/s; 520 vector instructions a wavefront keep it above the 45 of a copy), reading 34 (6.1 TB/s).
+// takes 49 us of that (4.3 TB/s; 520 vector instructions a wavefront keep it above the 44 of a copy), reading 34 (6.1 TB/s).
+// Rows in slots without order touch some eight lines each for their 144 bytes: 65536 of them 83 and 65 us, in pages 42 and 29.
 #include "common.h"
 #include "mpic_q4.h"
 #include "q4.h"

@@ -196,7 +196,7 @@ __device__ inline typename Held<T, D>::pairs pairs_in(const char* unit, int b, i
 
 // Direct loads of 1024 and 2 x 1024 contiguous bytes to LDS, 16 a lane: base in scalar registers, the lane's offset in one
 // vector register (an instruction's offset moves both addresses).  No compiler-visible load: the wait is by hand.
-// Non-temporal: a decode step reads its contexts once (24 contexts, 442 MB: loads alone 107 -> 98 us).
+// Non-temporal: a decode step reads its contexts once (24 contexts, 421 MB: 82 us, 90 with ordinary loads).
 __device__ inline void stage_1k(const char* base, uint32_t offset, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt" : : "v"(offset), "s"(base), "s"(lds) : "memory", "m0");
 }
